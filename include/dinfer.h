@@ -302,6 +302,115 @@ int dinfer_kv_write(dinfer_ctx* ctx, int32_t layer, const int32_t* d_page_row, i
 int dinfer_kv_read(dinfer_ctx* ctx, int32_t layer, const int32_t* d_page_row, int32_t first_pos, int32_t n_pos,
                    float* d_k, float* d_v, void* stream);
 
+/* ---- Operators on the paged cache ------------------------------------------------------------------------------
+ * For programs that run layers of their own on a context's cache (other norms, rotations or query heads than the step's),
+ * verify drafts, or shorten a long prefix.  A layer's new tokens are written with dinfer_kv_append, read with dinfer_attend,
+ * the attention that cached positions gather is summed with dinfer_kv_score, and dinfer_kv_evict moves the positions worth
+ * keeping into other pages.  dinfer_step_scored and dinfer_refresh_block_scored are the step over such a cache.
+ *
+ * Shared conventions.  n_seq <= max_seqs sequences; h_lens [n_seq] (host) new tokens of each, 0 allowed; the tokens are
+ * packed back to back, T = sum of h_lens rows.  Sequence s's tokens take the cache positions d_past[s] ..
+ * d_past[s]+h_lens[s]-1 (d_past null: from 0), through row s of d_page_table; a past that would leave max_pos or the page-table
+ * row is pulled back.  All row matrices hold the configuration's dtype, are 16-byte aligned, and their strides (elements
+ * between rows) are multiples of 16 bytes.  n_q_heads: query heads, a multiple of the configuration's n_heads; query head i
+ * belongs to cache head i / (n_q_heads / n_heads).  `layer` chooses the part of the pool.  The context must be used
+ * with the GPU that was current at dinfer_create (DINFER_EINVAL otherwise).  Sums, statistics and angles are float32 or
+ * wider; outputs are rounded once. */
+
+/* A rotation of the first rotary_dim features of a head (even, at most head_dim; the others pass through): pairs
+ * (j, j + rotary_dim/2), or (2j, 2j+1) with interleaved != 0, turn by position * f_j, f_j = theta^(-2j/rotary_dim) changed by
+ *   DINFER_ROTARY_PLAIN   nothing
+ *   DINFER_ROTARY_LINEAR  f_j / factor
+ *   DINFER_ROTARY_NTK     theta * factor^(r/(r-2)) in theta's place, r = rotary_dim > 2
+ *   DINFER_ROTARY_YARN    f_j for pairs that turn often within original_positions, f_j / factor for those that hardly turn, a linear ramp in j
+ *                         between: from low = floor(c(beta_fast)) (at least 0) to high = ceil(c(beta_slow)) (at most r - 1),
+ *                         c(b) = r ln(original_positions / (2 pi b)) / (2 ln theta); cosines and sines times magnitude
+ *                         (0: 0.1 ln(factor) + 1; 1 for the other kinds).
+ * beta_fast and beta_slow 0: 32 and 1. */
+enum { DINFER_ROTARY_PLAIN = 0, DINFER_ROTARY_LINEAR = 1, DINFER_ROTARY_NTK = 2, DINFER_ROTARY_YARN = 3 };
+typedef struct {
+  int32_t rotary_dim, interleaved, scaling, original_positions;
+  float theta, factor, beta_fast, beta_slow, magnitude;
+} dinfer_rotary;
+
+/* Cosines and sines of positions 0 .. max_pos-1, built once by the caller's program and kept: bytes (0: bad rotation), and
+ * the kernel that fills them (float32, angles in double). */
+size_t dinfer_rotary_table_bytes(const dinfer_rotary* rotary, int32_t max_pos);
+int dinfer_rotary_table(const dinfer_rotary* rotary, int32_t max_pos, void* d_table, size_t bytes, void* stream);
+
+/* Writes the keys and values of new tokens into the cache, and rotates their queries, in one pass:
+ *   d_q, d_k, d_v   rows of n_q_heads | n_heads | n_heads heads with strides of their own (parts of one fused matrix are fine).
+ *                   d_q may be null: keys and values only.
+ *   d_q_gain, d_k_gain [head_dim] float32: RMS norm of every head, x / sqrt(mean(x^2) + eps) * gain, in front of the rotation; null: none.
+ *   rotary, d_table the rotation and its table of table_positions rows (dinfer_rotary_table); rotary null: the
+ *                   context's own (whole head, rotate-half, the configuration's theta).
+ *   d_positions     [T] rotary positions, null: the cache positions.  Clamped to the table.
+ *   d_q_out         [T] rows of n_q_heads heads; may be d_q itself with the same stride. */
+int dinfer_kv_append(dinfer_ctx* ctx, int32_t layer, int32_t n_seq, const int32_t* h_lens, const int32_t* d_past,
+                     const int32_t* d_page_table, int32_t pt_stride, const void* d_q, int64_t q_stride, const void* d_k,
+                     int64_t k_stride, const void* d_v, int64_t v_stride, int32_t n_q_heads, const float* d_q_gain,
+                     const float* d_k_gain, float eps, const dinfer_rotary* rotary, const void* d_table,
+                     int32_t table_positions, const int32_t* d_positions, void* d_q_out, int64_t q_out_stride, void* stream);
+
+/* Attention of new tokens over the d_past[s] positions in front of them and over each other (their keys and values are in
+ * the cache already: dinfer_kv_append).
+ *   d_visible  [T] or null (every token sees all new tokens): bit j set = the token sees its sequence's new token j.  A tree of
+ *              drafts, a causal run, or padding that nobody sees; needs h_lens[s] <= 64.  What lies in keys and values a token does not
+ *              see, infinities and NaN included, does not reach it.  A token that sees nothing gets zeros.
+ *   scale      of the scores; 0: 1/sqrt(head_dim).
+ *   d_out      [T] rows of n_q_heads heads.
+ *   d_lse      [T][n_q_heads] float32, or null: logarithm of every row's sum of exponentials (-infinity: sees nothing). */
+int dinfer_attend(dinfer_ctx* ctx, int32_t layer, int32_t n_seq, const int32_t* h_lens, const int32_t* d_past,
+                  const int32_t* d_page_table, int32_t pt_stride, const void* d_q, int64_t q_stride, int32_t n_q_heads,
+                  const uint64_t* d_visible, float scale, void* d_out, int64_t out_stride, float* d_lse, void* stream);
+
+/* The attention weight that positions gather: for every cache head and position j < d_past[s]+h_lens[s] (and < score_stride),
+ *   d_score_out[s][head][j] = decay * d_score_in[s][head][j] + sum of softmax weights of j over the sequence's new tokens and
+ * the head's query heads.  d_score_in null: 0; it may be d_score_out.  Both [n_seq][n_heads][score_stride] float32; other
+ * entries, and sequences without new tokens, are left alone.
+ *   d_lse      [T][n_q_heads] float32: with lse_given != 0 what dinfer_attend left for the same arguments; with 0 it is worked
+ *              out first (one more pass over the keys) and left there.
+ * Every entry has one writer and a fixed order of additions: the same bits every time. */
+int dinfer_kv_score(dinfer_ctx* ctx, int32_t layer, int32_t n_seq, const int32_t* h_lens, const int32_t* d_past,
+                    const int32_t* d_page_table, int32_t pt_stride, const void* d_q, int64_t q_stride, int32_t n_q_heads,
+                    const uint64_t* d_visible, float scale, float* d_lse, int32_t lse_given, float decay,
+                    const float* d_score_in, float* d_score_out, int32_t score_stride, void* stream);
+
+/* Shortens the cache of n_seq sequences in layers first_layer .. first_layer+n_layers-1: every (layer, head) keeps its own
+ * `keep` positions of d_len[s] (all, if there are no more), in their order: the first n_sink, the last n_recent, and the ones
+ * of the best scores (n_sink + n_recent <= keep; equal scores: the lower position; NaN is below everything).  Their rows are
+ * copied, keys as rotated, to positions 0 .. of the pages in d_new_page_table, which must be pages that none of the
+ * call's old rows uses; every other row of the pool stays.
+ *   d_score [n_layers][n_seq][n_heads][score_stride] float32; positions from score_stride on are dropped.
+ *   d_kept  [n_layers][n_seq][n_heads][keep] out: the positions kept, ascending, then -1.
+ *   d_score_out  as d_score (another buffer), or null: their scores, then zeros.
+ *   d_new_len [n_seq] out: positions that are cached now (may not be d_len). */
+int dinfer_kv_evict(dinfer_ctx* ctx, int32_t first_layer, int32_t n_layers, int32_t n_seq, int32_t keep, int32_t n_sink,
+                    int32_t n_recent, const float* d_score, int32_t score_stride, const int32_t* d_len,
+                    const int32_t* d_page_table, int32_t pt_stride, const int32_t* d_new_page_table, int32_t new_pt_stride,
+                    int32_t* d_kept, float* d_score_out, int32_t* d_new_len, void* stream);
+
+/* dinfer_step and dinfer_refresh_block over a cache that may have been shortened, leaving scores:
+ *   d_position  [n_seq] or null: rotary position of the block's first token where it is not d_prefix_len[s] (the number of
+ *               cached positions); clamped so that the block stays inside max_pos.  dinfer_refresh_block_scored adds block_len to it.
+ *   d_score_out [n_layers][n_seq][n_heads][score_stride] float32 or null: every layer's dinfer_kv_score of the block's queries
+ *               (bidirectional, no visibility words), from d_score_in (null: 0) with decay.
+ * A step's scores cover the block's own positions as well. */
+typedef struct {
+  int32_t* d_position;
+  const float* d_score_in;
+  float* d_score_out;
+  int32_t score_stride;
+  float decay;
+} dinfer_cache_use;
+int dinfer_step_scored(dinfer_ctx* ctx, int32_t n_seq, int32_t block_len, int32_t* d_block_tokens, uint64_t* d_mask,
+                       const int32_t* d_prefix_len, const int32_t* d_page_table, int32_t pt_stride,
+                       const dinfer_decode* decode, const dinfer_cache_use* use, float* d_conf, int32_t* d_argmax,
+                       int32_t* d_n_committed, void* stream);
+int dinfer_refresh_block_scored(dinfer_ctx* ctx, int32_t n_seq, int32_t block_len, const int32_t* d_block_tokens,
+                                int32_t* d_prefix_len, const int32_t* d_page_table, int32_t pt_stride,
+                                const dinfer_cache_use* use, void* stream);
+
 /* Test hooks.  dinfer_debug_logits recomputes the logits of the last forward's rows (n_rows must equal their
  * number) through the LM-head kernel's arithmetic and stores them: d_out [n_rows][vocab] float32.  dinfer_debug_get copies
  * an intermediate of the last forward: what = 0 residual stream leaving the last layer [T][hidden] f32;

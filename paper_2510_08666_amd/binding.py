@@ -13,6 +13,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("DINFER_LIB") or os.path.join(_HERE, "libdinfer.so")   # DINFER_LIB: another build of it
 
 c_i32, c_u64, c_f32, c_vp, c_sz = ctypes.c_int32, ctypes.c_uint64, ctypes.c_float, ctypes.c_void_p, ctypes.c_size_t
+c_i64 = ctypes.c_int64
 
 F32, BF16 = 0, 1
 (T_EMB, T_LM_HEAD, T_FINAL_GAIN, T_ATTN_GAIN, T_WQ, T_WK, T_WV, T_WO, T_FFN_GAIN, T_ROUTER, T_GATE, T_UP,
@@ -26,7 +27,9 @@ EXPORTS = ["dinfer_weights_bytes", "dinfer_kv_bytes", "dinfer_workspace_bytes", 
            "dinfer_refresh_block", "dinfer_commit", "dinfer_generate",
            "dinfer_generate_block", "dinfer_kv_write", "dinfer_kv_read", "dinfer_debug_logits", "dinfer_debug_get",
            "dinfer_profile_every", "dinfer_profile_start", "dinfer_profile_stop", "dinfer_stream_read", "dinfer_debug_trace",
-           "dinfer_debug_single_slice", "dinfer_generate_block_smooth"]
+           "dinfer_debug_single_slice", "dinfer_generate_block_smooth", "dinfer_rotary_table_bytes", "dinfer_rotary_table",
+           "dinfer_kv_append", "dinfer_attend", "dinfer_kv_score", "dinfer_kv_evict", "dinfer_step_scored",
+           "dinfer_refresh_block_scored"]
 (STAGE_QKV, STAGE_ATTENTION, STAGE_OPROJ, STAGE_EXPERT_GATE_UP, STAGE_EXPERT_DOWN, STAGE_LM_HEAD,
  STAGE_ROUTER) = range(7)
 
@@ -61,6 +64,35 @@ class Credit(ctypes.Structure):
 class SmoothSchedule(ctypes.Structure):
     _fields_ = [("alpha_init", c_f32), ("alpha_growth", c_f32), ("alpha_preset", c_f32), ("threshold_start", c_f32),
                 ("threshold_decay", c_f32)]
+
+
+class Rotary(ctypes.Structure):
+    _fields_ = [(n, c_i32) for n in ("rotary_dim", "interleaved", "scaling", "original_positions")] + \
+               [(n, c_f32) for n in ("theta", "factor", "beta_fast", "beta_slow", "magnitude")]
+
+
+class CacheUse(ctypes.Structure):
+    _fields_ = [("d_position", c_vp), ("d_score_in", c_vp), ("d_score_out", c_vp), ("score_stride", c_i32), ("decay", c_f32)]
+
+
+ROTARY_SCALINGS = {"plain": 0, "linear": 1, "ntk": 2, "yarn": 3}
+
+
+def rotary(rotary_dim, interleaved=False, theta=10000.0, scaling="plain", factor=1.0, original_positions=0, beta_fast=0.0,
+           beta_slow=0.0, magnitude=0.0):
+    """A rotation of the first rotary_dim features of a head (see dinfer_rotary)."""
+    return Rotary(int(rotary_dim), int(bool(interleaved)), ROTARY_SCALINGS[scaling], int(original_positions), float(theta),
+                  float(factor), float(beta_fast), float(beta_slow), float(magnitude))
+
+
+def rotary_table(rot, max_pos, device="cuda:0"):
+    """Cosines and sines of positions 0 .. max_pos-1 as a [2][max_pos][rotary_dim / 2] device tensor."""
+    n = lib.dinfer_rotary_table_bytes(ctypes.byref(rot), int(max_pos))
+    if n == 0:
+        raise DinferError(-1, last_error())
+    t = torch.empty((2, int(max_pos), rot.rotary_dim // 2), dtype=torch.float32, device=device)
+    _check(lib.dinfer_rotary_table(ctypes.byref(rot), int(max_pos), _ptr(t), n, _stream()))
+    return t
 
 
 CREDIT_CAP = 64
@@ -126,6 +158,27 @@ def _load():
     L.dinfer_generate_block.restype = c_i32
     L.dinfer_generate_block.argtypes = [c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp, c_i32, P(Decode), c_vp, c_vp, c_vp,
                                         c_i32, c_i32, c_i32, P(c_i32), c_vp]
+    L.dinfer_rotary_table_bytes.restype = c_sz
+    L.dinfer_rotary_table_bytes.argtypes = [P(Rotary), c_i32]
+    L.dinfer_rotary_table.restype = c_i32
+    L.dinfer_rotary_table.argtypes = [P(Rotary), c_i32, c_vp, c_sz, c_vp]
+    L.dinfer_kv_append.restype = c_i32
+    L.dinfer_kv_append.argtypes = [c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, c_i32, c_vp, c_i64, c_vp, c_i64, c_vp, c_i64, c_i32,
+                                   c_vp, c_vp, c_f32, P(Rotary), c_vp, c_i32, c_vp, c_vp, c_i64, c_vp]
+    L.dinfer_attend.restype = c_i32
+    L.dinfer_attend.argtypes = [c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, c_i32, c_vp, c_i64, c_i32, c_vp, c_f32, c_vp, c_i64,
+                                c_vp, c_vp]
+    L.dinfer_kv_score.restype = c_i32
+    L.dinfer_kv_score.argtypes = [c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, c_i32, c_vp, c_i64, c_i32, c_vp, c_f32, c_vp, c_i32,
+                                  c_f32, c_vp, c_vp, c_i32, c_vp]
+    L.dinfer_kv_evict.restype = c_i32
+    L.dinfer_kv_evict.argtypes = [c_vp, c_i32, c_i32, c_i32, c_i32, c_i32, c_i32, c_vp, c_i32, c_vp, c_vp, c_i32, c_vp, c_i32,
+                                  c_vp, c_vp, c_vp, c_vp]
+    L.dinfer_step_scored.restype = c_i32
+    L.dinfer_step_scored.argtypes = [c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp, c_i32, P(Decode), P(CacheUse), c_vp, c_vp,
+                                     c_vp, c_vp]
+    L.dinfer_refresh_block_scored.restype = c_i32
+    L.dinfer_refresh_block_scored.argtypes = [c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, c_i32, P(CacheUse), c_vp]
     L.dinfer_commit.restype = c_i32
     L.dinfer_commit.argtypes = [c_vp, c_vp, c_i32, c_i32, c_vp, c_vp, P(Decode), c_vp, c_vp]
     L.dinfer_generate.restype = c_i32
@@ -214,6 +267,7 @@ class Context:
         if wb == 0 or kb == 0 or sb == 0:
             raise DinferError(-1, last_error())
         self.n_pages, self.max_seqs, self.max_tokens = n_pages, max_seqs, max_tokens
+        self._dtype = torch.bfloat16 if self.ccfg.dtype == BF16 else torch.float32
         if weights_buffer is not None:
             if weights_buffer.numel() < wb or weights_buffer.device != self.device:
                 raise ValueError("weights_buffer does not fit this configuration")
@@ -361,6 +415,73 @@ class Context:
                                    int(eos_id), int(steps_per_wait), _ptr(d_finished), _ptr(d_conf), _ptr(d_argmax),
                                    _ptr(d_n_committed), ctypes.byref(run), _stream()))
         return run.value
+
+    # ---- operators on the paged cache (shapes: T = sum(lens) rows; see include/dinfer.h)
+    def _rows(self, name, t, heads):
+        """Address and stride of a [T][heads * head_dim] matrix, rows contiguous."""
+        if t.dtype is not self._dtype or t.dim() != 2 or t.shape[1] != heads * self.cfg.head_dim or t.stride(1) != 1:
+            raise ValueError("%s must be a [T][%d] tensor of the context's dtype with contiguous rows" % (name, heads * self.cfg.head_dim))
+        return t.data_ptr(), t.stride(0)
+
+    def kv_append(self, layer, lens, d_past, d_page_table, d_q, d_k, d_v, d_q_out, q_gain=None, k_gain=None, eps=1e-6,
+                  rotary=None, rotary_table=None, positions=None):
+        """Norms, rotates and stores a layer's new tokens; d_q_out receives the queries (d_q and d_q_out None: keys and values only)."""
+        n, nh = len(lens), self.cfg.n_heads
+        k, v = self._rows("d_k", d_k, nh), self._rows("d_v", d_v, nh)
+        nq = nh if d_q is None else d_q.shape[1] // self.cfg.head_dim
+        q, out = ((None, 0), (None, 0)) if d_q is None else (self._rows("d_q", d_q, nq), self._rows("d_q_out", d_q_out, nq))
+        _check(lib.dinfer_kv_append(self.h, layer, n, (c_i32 * n)(*lens), _ptr(d_past), _ptr(d_page_table), d_page_table.shape[1],
+                                    q[0], q[1], k[0], k[1], v[0], v[1], nq, _ptr(q_gain), _ptr(k_gain), eps, rotary,
+                                    _ptr(rotary_table), 0 if rotary_table is None else rotary_table.shape[1], _ptr(positions),
+                                    out[0], out[1], _stream()))
+
+    def attend(self, layer, lens, d_past, d_page_table, d_q, d_out, visible=None, scale=0.0, lse=None):
+        """Attention of the new tokens over the cache, their own keys as far as the words of `visible` [T] allow."""
+        n, nq = len(lens), d_q.shape[1] // self.cfg.head_dim
+        q, out = self._rows("d_q", d_q, nq), self._rows("d_out", d_out, nq)
+        _check(lib.dinfer_attend(self.h, layer, n, (c_i32 * n)(*lens), _ptr(d_past), _ptr(d_page_table), d_page_table.shape[1],
+                                 q[0], q[1], nq, _ptr(visible), scale, out[0], out[1], _ptr(lse), _stream()))
+
+    def kv_score(self, layer, lens, d_past, d_page_table, d_q, d_score_out, score_in=None, decay=1.0, visible=None, scale=0.0,
+                 lse=None):
+        """Adds the attention weight of the new tokens to d_score_out [n_seq][n_heads][stride]; lse: what `attend` left for
+        the same queries (None: worked out here)."""
+        n, nq = len(lens), d_q.shape[1] // self.cfg.head_dim
+        q = self._rows("d_q", d_q, nq)
+        given = lse is not None
+        if not given:
+            lse = torch.empty((d_q.shape[0], nq), dtype=torch.float32, device=d_q.device)
+        _check(lib.dinfer_kv_score(self.h, layer, n, (c_i32 * n)(*lens), _ptr(d_past), _ptr(d_page_table), d_page_table.shape[1],
+                                   q[0], q[1], nq, _ptr(visible), scale, _ptr(lse), given, decay, _ptr(score_in),
+                                   _ptr(d_score_out), d_score_out.shape[2], _stream()))
+
+    def kv_evict(self, first_layer, n_layers, keep, n_sink, n_recent, d_score, d_len, d_page_table, d_new_page_table, d_kept,
+                 d_new_len, score_out=None):
+        """Keeps `keep` positions per (layer, sequence, head) of d_score [n_layers][n_seq][n_heads][stride] in new pages."""
+        _check(lib.dinfer_kv_evict(self.h, first_layer, n_layers, d_page_table.shape[0], keep, n_sink, n_recent, _ptr(d_score),
+                                   d_score.shape[3], _ptr(d_len), _ptr(d_page_table), d_page_table.shape[1],
+                                   _ptr(d_new_page_table), d_new_page_table.shape[1], _ptr(d_kept), _ptr(score_out),
+                                   _ptr(d_new_len), _stream()))
+
+    @staticmethod
+    def _cache_use(position, score_in, score_out, decay):
+        return CacheUse(_ptr(position), _ptr(score_in), _ptr(score_out), 0 if score_out is None else score_out.shape[3], decay)
+
+    def step_scored(self, d_block_tokens, d_mask, d_prefix_len, d_page_table, threshold, fixed_k, d_conf, d_argmax,
+                    d_n_committed, position=None, score_in=None, score_out=None, decay=1.0):
+        """step over a cache that may have been shortened; score_out [n_layers][n_seq][n_heads][stride] receives its scores."""
+        n_seq, block_len = d_block_tokens.shape
+        dec, use = _decode(threshold, fixed_k), self._cache_use(position, score_in, score_out, decay)
+        _check(lib.dinfer_step_scored(self.h, n_seq, block_len, _ptr(d_block_tokens), _ptr(d_mask), _ptr(d_prefix_len),
+                                      _ptr(d_page_table), d_page_table.shape[1], ctypes.byref(dec), ctypes.byref(use),
+                                      _ptr(d_conf), _ptr(d_argmax), _ptr(d_n_committed), _stream()))
+
+    def refresh_block_scored(self, d_block_tokens, d_prefix_len, d_page_table, position=None, score_in=None, score_out=None,
+                             decay=1.0):
+        n_seq, block_len = d_block_tokens.shape
+        use = self._cache_use(position, score_in, score_out, decay)
+        _check(lib.dinfer_refresh_block_scored(self.h, n_seq, block_len, _ptr(d_block_tokens), _ptr(d_prefix_len),
+                                               _ptr(d_page_table), d_page_table.shape[1], ctypes.byref(use), _stream()))
 
     # ---- KV rows in and out, test hooks
     def kv_write(self, layer, d_page_row, first_pos, d_k, d_v):

@@ -1,6 +1,7 @@
 // C-ABI of the dinfer library: argument checks, buffer carving, and the launch sequence of one forward.
 #include "../../include/dinfer.h"
 
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 #include <string.h>
@@ -8,6 +9,7 @@
 #include <new>
 #include <vector>
 
+#include "cache.hpp"
 #include "gemm.hpp"
 #include "kernels.hpp"
 
@@ -138,7 +140,8 @@ int attn_splits(int n_qtiles, int n_heads, int key_bound) {
 
 struct Workspace {
   size_t cos_tab, sin_tab, tok_seq, tok_pos, seq_nkeys, qtile, x, xn, xn_hi, ssq, ssq_a, tk_part, tickets, tickets_bytes, attn_tickets, attn_tickets_bytes, rinv_f, q, a, attn_part, topk_idx, topk_w, cnt, off,
-      perm, shares, work, hist, run_tokens, run_base, n_finished, loop_flags, loop_steps, lm_rows, y, o, lm_part, smooth_part, lm_stats, conf, argmax, total;
+      perm, shares, work, hist, run_tokens, run_base, n_finished, loop_flags, loop_steps, lm_rows, y, o, lm_part, smooth_part, lm_stats, conf, argmax,
+      tok_rot, attend_part, attend_tickets, score_lse, total;
 };
 
 Workspace map_workspace(const dinfer_config& c, int max_seqs, int max_tokens) {
@@ -211,6 +214,10 @@ Workspace map_workspace(const dinfer_config& c, int max_seqs, int max_tokens) {
   w.lm_stats = cv.take(T * 2 * 4);
   w.conf = cv.take(T * 4);
   w.argmax = cv.take(T * 4);
+  w.tok_rot = cv.take(T * 4);                    // rotary positions of a forward over a shortened cache
+  w.attend_part = cv.take(attend_part_bytes(c.head_dim));
+  w.attend_tickets = cv.take((size_t)ATTEND_MAX_SHARED * 4);
+  w.score_lse = cv.take(T * c.n_heads * 4);      // normalisers of a scored step's rows
   w.total = cv.at;
   return w;
 }
@@ -280,10 +287,30 @@ struct StageTimer {
   }
 };
 
+// The attention weight of a forward's queries, which are in the workspace, added to layer l's scores.
+void score_layer(dinfer_ctx* c, const SeqSpan& span, const int32_t* d_base, int limit, const int32_t* d_page_table, int pt_stride,
+                 int l, const dinfer_cache_use& use, hipStream_t st) {
+  const dinfer_config& f = c->cfg;
+  const int D = f.n_heads * f.head_dim, planes = c->bf16 ? 2 : 1;
+  const int64_t q_plane = (int64_t)c->max_tokens * D;
+  const void* kv_layer = c->kv + (size_t)l * c->kv_layer_bytes;
+  const CacheTokens tok{span, d_base, limit, d_page_table, pt_stride};
+  const float scale = 1.f / sqrtf((float)f.head_dim);
+  float* lse = at<float>(c->ws, c->wsm.score_lse);
+  AttendArgs aa{tok, {}, kv_layer, c->geom, c->ws + c->wsm.q, D, q_plane, 1, nullptr, scale, nullptr, 0, lse,
+                at<float>(c->ws, c->wsm.attend_part), at<int32_t>(c->ws, c->wsm.attend_tickets)};
+  fill_tiles(span, 1, &aa.tiles);
+  launch_attend(c->bf16, planes, aa, st);
+  const int64_t layer_scores = (int64_t)span.n_seq * f.n_heads * use.score_stride * l;
+  launch_score(c->bf16, planes,
+               ScoreArgs{tok, kv_layer, c->geom, c->ws + c->wsm.q, D, q_plane, 1, nullptr, scale, lse, use.decay,
+                         use.d_score_in ? use.d_score_in + layer_scores : nullptr, use.d_score_out + layer_scores, use.score_stride}, st);
+}
+
 // One forward over the packed tokens of `span`.  with_head: an LM head follows (LmArgs::xn_hi is wanted).
 int forward(dinfer_ctx* c, const SeqSpan& span, const int32_t* d_tokens, const int32_t* d_base,
             const int32_t* d_page_table, int pt_stride, bool with_head, hipStream_t st,
-            const SmoothIn* smooth = nullptr) {
+            const SmoothIn* smooth = nullptr, const dinfer_cache_use* use = nullptr) {
   const dinfer_config& f = c->cfg;
   const bool bf = c->bf16;
   const int T = span.off[span.n_seq];
@@ -293,8 +320,10 @@ int forward(dinfer_ctx* c, const SeqSpan& span, const int32_t* d_tokens, const i
   if (c->prof_stage >= 0) c->prof_sampled = c->prof_fwd++ % c->prof_every == 0;
   int n_qtiles = 0;
   for (int s = 0; s < span.n_seq; ++s) n_qtiles += (span.off[s + 1] - span.off[s] + TILE - 1) / TILE;
-  FwdMeta meta{at<int32_t>(ws, w.tok_seq), at<int32_t>(ws, w.tok_pos), at<int32_t>(ws, w.seq_nkeys),
-               at<int32_t>(ws, w.qtile)};
+  const bool moved = use && use->d_position, scored = use && use->d_score_out;
+  const RotaryStart rot{moved ? use->d_position : nullptr, f.max_pos, at<int32_t>(ws, w.tok_rot)};
+  FwdMeta meta{at<int32_t>(ws, w.tok_seq), at<int32_t>(ws, w.tok_pos), at<int32_t>(ws, moved ? w.tok_rot : w.tok_pos),
+               at<int32_t>(ws, w.seq_nkeys), at<int32_t>(ws, w.qtile)};
   const int limit = f.max_pos < pt_stride * PAGE ? f.max_pos : pt_stride * PAGE;
   float* x = at<float>(ws, w.x);
   float* ssq_a = at<float>(ws, w.ssq_a);
@@ -320,7 +349,7 @@ int forward(dinfer_ctx* c, const SeqSpan& span, const int32_t* d_tokens, const i
     if (l == 0)
       launch_embed(bf, d_tokens, c->weights + c->wm.emb, T, H, f.vocab, x, ssq_a, at<float>(c->weights, lw.attn_gain),
                    xn, smooth, span, d_base, limit, at<int32_t>(ws, w.tok_seq), at<int32_t>(ws, w.tok_pos),
-                   at<int32_t>(ws, w.seq_nkeys), at<int32_t>(ws, w.qtile), st);
+                   at<int32_t>(ws, w.seq_nkeys), at<int32_t>(ws, w.qtile), rot, st);
     else if (!fused_down)
       launch_combine(bf, x, at<float>(ws, w.o), topk_w - (size_t)T * f.top_k, f.top_k, T, H, ssq_a,
                      at<float>(c->weights, lw.attn_gain), xn, st);
@@ -340,6 +369,7 @@ int forward(dinfer_ctx* c, const SeqSpan& span, const int32_t* d_tokens, const i
       StageTimer tm(c, DINFER_STAGE_ATTENTION, st);
       launch_attention(bf, aa, st);
     }
+    if (scored) score_layer(c, span, d_base, limit, d_page_table, pt_stride, l, *use, st);
     OprojArgs oa{c->weights + lw.wo, ws + w.a, x, at<float>(c->weights, lw.ffn_gain), xn,
                  at<float>(ws, w.ssq), T, D, H, tk_part, tickets, share_features ? c->weights + lw.router : nullptr, at<float>(ws, w.shares), share_features};
     {
@@ -492,7 +522,7 @@ int dinfer_create(const dinfer_config* cfg, void* d_weights, size_t weights_byte
     delete c;
     return fail(DINFER_EHIP, "hipHostMalloc failed");
   }
-  if (!configure_kernels() || !configure_attention() || !configure_wide()) {
+  if (!configure_kernels() || !configure_attention() || !configure_wide() || !configure_attend()) {
     (void)hipHostFree(c->h_mask_pinned);
     delete c;
     return fail(DINFER_EHIP, "the runtime refused the kernels' LDS sizes");
@@ -500,6 +530,7 @@ int dinfer_create(const dinfer_config* cfg, void* d_weights, size_t weights_byte
   // the arrival counters start at zero and every kernel that uses them leaves them at zero
   if (hipMemsetAsync(c->ws + c->wsm.tickets, 0, c->wsm.tickets_bytes, (hipStream_t)stream) != hipSuccess ||
       hipMemsetAsync(c->ws + c->wsm.attn_tickets, 0, c->wsm.attn_tickets_bytes, (hipStream_t)stream) != hipSuccess ||
+      hipMemsetAsync(c->ws + c->wsm.attend_tickets, 0, (size_t)ATTEND_MAX_SHARED * 4, (hipStream_t)stream) != hipSuccess ||
       hipMemsetAsync(c->ws + c->wsm.off, 0, (size_t)OFF_INTS * 4, (hipStream_t)stream) != hipSuccess) {
     (void)hipHostFree(c->h_mask_pinned);
     delete c;
@@ -595,13 +626,14 @@ int dinfer_prefill(dinfer_ctx* c, int32_t n_seq, const int32_t* d_tokens, const 
 static int step_impl(dinfer_ctx* c, int32_t n_seq, int32_t block_len, int32_t* d_block_tokens, uint64_t* d_mask,
                      const int32_t* d_prefix_len, const int32_t* d_page_table, int32_t pt_stride,
                      const dinfer_decode* decode, float* d_conf, int32_t* d_argmax, int32_t* d_n_committed,
-                     hipStream_t st, const int32_t* live, int32_t* next_live, int32_t* steps) {
+                     hipStream_t st, const int32_t* live, int32_t* next_live, int32_t* steps,
+                     const dinfer_cache_use* use = nullptr) {
   int rc = check_block_args(c, n_seq, block_len, d_block_tokens, d_prefix_len, d_page_table, pt_stride);
   if (rc != DINFER_OK) return rc;
   if (!d_mask || !decode || !d_conf || !d_argmax || !d_n_committed) return fail(DINFER_EINVAL, "null pointer");
   if ((rc = check_decode(decode)) != DINFER_OK) return rc;
   LiveScope scope(live);
-  rc = forward(c, uniform_span(n_seq, block_len), d_block_tokens, d_prefix_len, d_page_table, pt_stride, true, st);
+  rc = forward(c, uniform_span(n_seq, block_len), d_block_tokens, d_prefix_len, d_page_table, pt_stride, true, st, nullptr, use);
   if (rc != DINFER_OK) return rc;
   const dinfer_config& f = c->cfg;
   const int T = n_seq * block_len;
@@ -972,6 +1004,277 @@ int dinfer_kv_write(dinfer_ctx* c, int32_t layer, const int32_t* d_page_row, int
 int dinfer_kv_read(dinfer_ctx* c, int32_t layer, const int32_t* d_page_row, int32_t first_pos, int32_t n_pos,
                    float* d_k, float* d_v, void* stream) {
   return kv_copy(c, false, layer, d_page_row, first_pos, n_pos, d_k, d_v, stream);
+}
+
+// ---- operators on the paged cache
+
+// Arguments that the operators share; fills tok.  T is tok->span.off[n_seq].
+static int cache_tokens(dinfer_ctx* c, int32_t layer, int32_t n_seq, const int32_t* h_lens, const int32_t* d_past,
+                        const int32_t* d_page_table, int32_t pt_stride, int32_t n_q_heads, CacheTokens* tok) {
+  if (!c) return fail(DINFER_EINVAL, "context is null");
+  if (!h_lens || !d_page_table) return fail(DINFER_EINVAL, "null pointer");
+  if (layer < 0 || layer >= c->cfg.n_layers) return fail(DINFER_EINVAL, "layer %d", layer);
+  if (n_seq < 1 || n_seq > c->max_seqs) return fail(DINFER_EINVAL, "n_seq %d outside [1, %d]", n_seq, c->max_seqs);
+  if (n_q_heads < c->cfg.n_heads || n_q_heads % c->cfg.n_heads || n_q_heads / c->cfg.n_heads > MAX_GROUP)
+    return fail(DINFER_EINVAL, "n_q_heads %d is no multiple of n_heads %d up to %d of them", n_q_heads, c->cfg.n_heads, MAX_GROUP);
+  if (pt_stride < 1) return fail(DINFER_ENOSPACE, "page table row too short");
+  const int64_t row = (int64_t)pt_stride * PAGE;
+  tok->limit = row < c->cfg.max_pos ? (int32_t)row : c->cfg.max_pos;
+  tok->past = d_past;
+  tok->page_table = d_page_table;
+  tok->pt_stride = pt_stride;
+  tok->span.n_seq = n_seq;
+  tok->span.off[0] = 0;
+  for (int s = 0; s < n_seq; ++s) {
+    if (h_lens[s] < 0) return fail(DINFER_EINVAL, "%d new tokens", h_lens[s]);
+    if (h_lens[s] > tok->limit)
+      return fail(DINFER_ENOSPACE, "%d new tokens exceed max_pos %d or the page-table row (%d pages)", h_lens[s], c->cfg.max_pos, pt_stride);
+    tok->span.off[s + 1] = tok->span.off[s] + h_lens[s];     // <= 64 * 32768
+  }
+  return DINFER_OK;
+}
+static int check_device(const dinfer_ctx* c) {
+  int dev = -1;
+  HIP_TRY(hipGetDevice(&dev));
+  if (dev != c->device) return fail(DINFER_EINVAL, "the context was created on device %d, the current device is %d", c->device, dev);
+  return DINFER_OK;
+}
+// A matrix of rows of `heads` heads: 16-byte aligned, its stride holding a row and a multiple of 16 bytes.
+static int check_rows(const dinfer_ctx* c, const char* name, const void* p, int64_t stride, int heads) {
+  if (!p) return fail(DINFER_EINVAL, "%s is null", name);
+  const int es = c->bf16 ? 2 : 4;
+  if (((uintptr_t)p & 15) || stride < (int64_t)heads * c->cfg.head_dim || stride * es % 16 || stride > INT32_MAX)
+    return fail(DINFER_EINVAL, "%s: 16-byte aligned rows, at least %d elements apart, a multiple of 16 bytes", name, heads * c->cfg.head_dim);
+  return DINFER_OK;
+}
+static int check_scale(const dinfer_ctx* c, float scale, float* out) {
+  if (!(scale >= 0.f && scale < INFINITY)) return fail(DINFER_EINVAL, "scale %g", (double)scale);
+  *out = scale > 0.f ? scale : 1.f / sqrtf((float)c->cfg.head_dim);
+  return DINFER_OK;
+}
+static int check_visible(const CacheTokens& tok, const uint64_t* d_visible) {
+  for (int s = 0; d_visible && s < tok.span.n_seq; ++s)
+    if (tok.span.off[s + 1] - tok.span.off[s] > 64)
+      return fail(DINFER_EINVAL, "visibility words reach 64 new tokens, sequence %d has %d", s, tok.span.off[s + 1] - tok.span.off[s]);
+  return DINFER_OK;
+}
+
+// Checks a rotation and works out what its table is built from.
+static int rotary_rule(const dinfer_rotary* r, RotaryRule* out) {
+  if (!r) return fail(DINFER_EINVAL, "rotary is null");
+  if (r->rotary_dim < 2 || r->rotary_dim % 2 || r->rotary_dim > 128) return fail(DINFER_EINVAL, "rotary_dim %d", r->rotary_dim);
+  if (r->scaling < DINFER_ROTARY_PLAIN || r->scaling > DINFER_ROTARY_YARN) return fail(DINFER_EINVAL, "scaling %d", r->scaling);
+  if (!(r->theta > 0.f && r->theta < INFINITY)) return fail(DINFER_EINVAL, "theta %g", (double)r->theta);
+  if (r->scaling != DINFER_ROTARY_PLAIN && !(r->factor > 0.f && r->factor < INFINITY)) return fail(DINFER_EINVAL, "factor %g", (double)r->factor);
+  const double n = r->rotary_dim;
+  *out = RotaryRule{r->rotary_dim, r->scaling, r->theta, r->factor, 0.0, 1.0, 1.0};
+  if (r->scaling == DINFER_ROTARY_NTK) {
+    if (r->rotary_dim == 2) return fail(DINFER_EINVAL, "a raised base needs rotary_dim > 2");
+    out->theta = r->theta * pow((double)r->factor, n / (n - 2));
+  }
+  if (r->scaling == DINFER_ROTARY_YARN) {
+    const double fast = r->beta_fast == 0.f ? 32.0 : r->beta_fast, slow = r->beta_slow == 0.f ? 1.0 : r->beta_slow;
+    if (!(fast >= slow && slow > 0.0 && fast < INFINITY) || r->original_positions < 1 || !(r->theta > 1.f) || !(r->magnitude >= 0.f && r->magnitude < INFINITY))
+      return fail(DINFER_EINVAL, "ramped frequencies: beta_fast >= beta_slow > 0, original_positions >= 1, theta > 1, magnitude >= 0");
+    const double two_pi = 6.283185307179586476925286766559;
+    const double lo = floor(n * log(r->original_positions / (fast * two_pi)) / (2 * log((double)r->theta)));
+    const double hi = ceil(n * log(r->original_positions / (slow * two_pi)) / (2 * log((double)r->theta)));
+    out->low = lo > 0 ? lo : 0;
+    out->high = hi < n - 1 ? hi : n - 1;
+    if (out->high - out->low < 0.001) out->high = out->low + 0.001;
+    out->magnitude = r->magnitude > 0.f ? r->magnitude : 0.1 * log((double)r->factor) + 1.0;
+  }
+  return DINFER_OK;
+}
+
+size_t dinfer_rotary_table_bytes(const dinfer_rotary* rotary, int32_t max_pos) {
+  RotaryRule rule;
+  if (rotary_rule(rotary, &rule) != DINFER_OK) return 0;
+  if (max_pos < 1 || max_pos > ATTN_MAX_PAGES * PAGE) {
+    (void)fail(DINFER_EINVAL, "max_pos %d outside [1, %d]", max_pos, ATTN_MAX_PAGES * PAGE);
+    return 0;
+  }
+  return (size_t)max_pos * rule.rotary_dim * 4;
+}
+
+int dinfer_rotary_table(const dinfer_rotary* rotary, int32_t max_pos, void* d_table, size_t bytes, void* stream) {
+  const size_t need = dinfer_rotary_table_bytes(rotary, max_pos);
+  if (need == 0) return DINFER_EINVAL;
+  if (!d_table || ((uintptr_t)d_table & 15)) return fail(DINFER_EINVAL, "the table must be 16-byte aligned device memory");
+  if (bytes < need) return fail(DINFER_ENOSPACE, "rotary table %zu < %zu bytes", bytes, need);
+  RotaryRule rule;
+  (void)rotary_rule(rotary, &rule);
+  float* cos_tab = (float*)d_table;
+  launch_rotary_table(rule, max_pos, cos_tab, cos_tab + (size_t)max_pos * (rule.rotary_dim / 2), (hipStream_t)stream);
+  HIP_TRY(hipGetLastError());
+  return DINFER_OK;
+}
+
+int dinfer_kv_append(dinfer_ctx* c, int32_t layer, int32_t n_seq, const int32_t* h_lens, const int32_t* d_past,
+                     const int32_t* d_page_table, int32_t pt_stride, const void* d_q, int64_t q_stride, const void* d_k,
+                     int64_t k_stride, const void* d_v, int64_t v_stride, int32_t n_q_heads, const float* d_q_gain,
+                     const float* d_k_gain, float eps, const dinfer_rotary* rotary, const void* d_table,
+                     int32_t table_positions, const int32_t* d_positions, void* d_q_out, int64_t q_out_stride, void* stream) {
+  AppendArgs a;
+  int rc = cache_tokens(c, layer, n_seq, h_lens, d_past, d_page_table, pt_stride, n_q_heads, &a.tok);
+  if (rc != DINFER_OK) return rc;
+  if ((rc = check_rows(c, "d_k", d_k, k_stride, c->cfg.n_heads)) != DINFER_OK) return rc;
+  if ((rc = check_rows(c, "d_v", d_v, v_stride, c->cfg.n_heads)) != DINFER_OK) return rc;
+  if (d_q) {
+    if ((rc = check_rows(c, "d_q", d_q, q_stride, n_q_heads)) != DINFER_OK) return rc;
+    if ((rc = check_rows(c, "d_q_out", d_q_out, q_out_stride, n_q_heads)) != DINFER_OK) return rc;
+    if (d_q_out == d_q && q_out_stride != q_stride) return fail(DINFER_EINVAL, "queries in place need one stride");
+  }
+  if ((d_q_gain || d_k_gain) && !(eps >= 0.f && eps < INFINITY)) return fail(DINFER_EINVAL, "eps %g", (double)eps);
+  if ((rc = check_device(c)) != DINFER_OK) return rc;
+  a.kv_layer = c->kv + (size_t)layer * c->kv_layer_bytes;
+  a.geom = c->geom;
+  a.q = d_q, a.k = d_k, a.v = d_v;
+  a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride;
+  a.group = n_q_heads / c->cfg.n_heads;
+  a.q_gain = d_q_gain, a.k_gain = d_k_gain, a.eps = eps;
+  if (rotary) {
+    RotaryRule rule;
+    if ((rc = rotary_rule(rotary, &rule)) != DINFER_OK) return rc;
+    if (rotary->rotary_dim > c->cfg.head_dim) return fail(DINFER_EINVAL, "rotary_dim %d exceeds head_dim", rotary->rotary_dim);
+    if (!d_table || ((uintptr_t)d_table & 15) || table_positions < 1 || table_positions > ATTN_MAX_PAGES * PAGE)
+      return fail(DINFER_EINVAL, "rotary table of %d positions", table_positions);
+    a.rotary_dim = rotary->rotary_dim, a.interleaved = rotary->interleaved != 0;
+    a.cos_tab = (const float*)d_table;
+    a.sin_tab = a.cos_tab + (size_t)table_positions * (rotary->rotary_dim / 2);
+    a.table_rows = table_positions;
+  } else {
+    a.rotary_dim = c->cfg.head_dim, a.interleaved = 0;
+    a.cos_tab = at<float>(c->ws, c->wsm.cos_tab);
+    a.sin_tab = at<float>(c->ws, c->wsm.sin_tab);
+    a.table_rows = c->cfg.max_pos;
+  }
+  a.positions = d_positions;
+  a.q_out = d_q_out, a.q_out_stride = q_out_stride;
+  if (a.tok.span.off[n_seq] == 0) return DINFER_OK;
+  launch_append(c->bf16, a, (hipStream_t)stream);
+  HIP_TRY(hipGetLastError());
+  return DINFER_OK;
+}
+
+int dinfer_attend(dinfer_ctx* c, int32_t layer, int32_t n_seq, const int32_t* h_lens, const int32_t* d_past,
+                  const int32_t* d_page_table, int32_t pt_stride, const void* d_q, int64_t q_stride, int32_t n_q_heads,
+                  const uint64_t* d_visible, float scale, void* d_out, int64_t out_stride, float* d_lse, void* stream) {
+  AttendArgs a;
+  int rc = cache_tokens(c, layer, n_seq, h_lens, d_past, d_page_table, pt_stride, n_q_heads, &a.tok);
+  if (rc != DINFER_OK) return rc;
+  if ((rc = check_rows(c, "d_q", d_q, q_stride, n_q_heads)) != DINFER_OK) return rc;
+  if ((rc = check_rows(c, "d_out", d_out, out_stride, n_q_heads)) != DINFER_OK) return rc;
+  if ((rc = check_visible(a.tok, d_visible)) != DINFER_OK) return rc;
+  if ((rc = check_scale(c, scale, &a.scale)) != DINFER_OK) return rc;
+  if ((rc = check_device(c)) != DINFER_OK) return rc;
+  a.group = n_q_heads / c->cfg.n_heads;
+  fill_tiles(a.tok.span, a.group, &a.tiles);
+  a.kv_layer = c->kv + (size_t)layer * c->kv_layer_bytes;
+  a.geom = c->geom;
+  a.q = d_q, a.q_stride = q_stride, a.q_plane = 0;
+  a.visible = d_visible;
+  a.out = d_out, a.out_stride = out_stride;
+  a.lse = d_lse;
+  a.part = at<float>(c->ws, c->wsm.attend_part);
+  a.tickets = at<int32_t>(c->ws, c->wsm.attend_tickets);
+  if (a.tok.span.off[n_seq] == 0) return DINFER_OK;
+  launch_attend(c->bf16, 1, a, (hipStream_t)stream);
+  HIP_TRY(hipGetLastError());
+  return DINFER_OK;
+}
+
+int dinfer_kv_score(dinfer_ctx* c, int32_t layer, int32_t n_seq, const int32_t* h_lens, const int32_t* d_past,
+                    const int32_t* d_page_table, int32_t pt_stride, const void* d_q, int64_t q_stride, int32_t n_q_heads,
+                    const uint64_t* d_visible, float scale, float* d_lse, int32_t lse_given, float decay,
+                    const float* d_score_in, float* d_score_out, int32_t score_stride, void* stream) {
+  ScoreArgs a;
+  int rc = cache_tokens(c, layer, n_seq, h_lens, d_past, d_page_table, pt_stride, n_q_heads, &a.tok);
+  if (rc != DINFER_OK) return rc;
+  if ((rc = check_rows(c, "d_q", d_q, q_stride, n_q_heads)) != DINFER_OK) return rc;
+  if (!d_lse || !d_score_out) return fail(DINFER_EINVAL, "null pointer");
+  if (score_stride < 1) return fail(DINFER_EINVAL, "score_stride %d", score_stride);
+  if (!(decay >= 0.f && decay < INFINITY)) return fail(DINFER_EINVAL, "decay %g", (double)decay);
+  if ((rc = check_visible(a.tok, d_visible)) != DINFER_OK) return rc;
+  if ((rc = check_scale(c, scale, &a.scale)) != DINFER_OK) return rc;
+  if ((rc = check_device(c)) != DINFER_OK) return rc;
+  a.group = n_q_heads / c->cfg.n_heads;
+  a.kv_layer = c->kv + (size_t)layer * c->kv_layer_bytes;
+  a.geom = c->geom;
+  a.q = d_q, a.q_stride = q_stride, a.q_plane = 0;
+  a.visible = d_visible;
+  a.lse = d_lse;
+  a.decay = decay;
+  a.score_in = d_score_in, a.score_out = d_score_out, a.score_stride = score_stride;
+  if (a.tok.span.off[n_seq] == 0) return DINFER_OK;
+  if (!lse_given) {
+    AttendArgs n{a.tok, {}, a.kv_layer, a.geom, d_q, q_stride, 0, a.group, d_visible, a.scale, nullptr, 0, d_lse,
+                 at<float>(c->ws, c->wsm.attend_part), at<int32_t>(c->ws, c->wsm.attend_tickets)};
+    fill_tiles(a.tok.span, a.group, &n.tiles);
+    launch_attend(c->bf16, 1, n, (hipStream_t)stream);
+  }
+  launch_score(c->bf16, 1, a, (hipStream_t)stream);
+  HIP_TRY(hipGetLastError());
+  return DINFER_OK;
+}
+
+int dinfer_kv_evict(dinfer_ctx* c, int32_t first_layer, int32_t n_layers, int32_t n_seq, int32_t keep, int32_t n_sink,
+                    int32_t n_recent, const float* d_score, int32_t score_stride, const int32_t* d_len,
+                    const int32_t* d_page_table, int32_t pt_stride, const int32_t* d_new_page_table, int32_t new_pt_stride,
+                    int32_t* d_kept, float* d_score_out, int32_t* d_new_len, void* stream) {
+  if (!c) return fail(DINFER_EINVAL, "context is null");
+  if (!d_score || !d_len || !d_page_table || !d_new_page_table || !d_kept || !d_new_len) return fail(DINFER_EINVAL, "null pointer");
+  if (first_layer < 0 || n_layers < 1 || n_layers > c->cfg.n_layers - first_layer)
+    return fail(DINFER_EINVAL, "layers %d and %d more", first_layer, n_layers);
+  if (n_seq < 1 || n_seq > c->max_seqs) return fail(DINFER_EINVAL, "n_seq %d outside [1, %d]", n_seq, c->max_seqs);
+  if (keep < 1 || keep > c->cfg.max_pos) return fail(DINFER_EINVAL, "keep %d outside [1, max_pos]", keep);
+  if (n_sink < 0 || n_recent < 0 || (int64_t)n_sink + n_recent > keep) return fail(DINFER_EINVAL, "n_sink %d and n_recent %d of keep %d", n_sink, n_recent, keep);
+  if (score_stride < 1) return fail(DINFER_EINVAL, "score_stride %d", score_stride);
+  if (pt_stride < 1 || (int64_t)new_pt_stride * PAGE < keep) return fail(DINFER_ENOSPACE, "page table row too short");
+  if (d_page_table == d_new_page_table) return fail(DINFER_EINVAL, "the new pages must be others than the old ones");
+  if (d_score_out == d_score || d_new_len == d_len) return fail(DINFER_EINVAL, "d_score_out and d_new_len must be other buffers than d_score and d_len");
+  int rc = check_device(c);
+  if (rc != DINFER_OK) return rc;
+  const int64_t row = (int64_t)pt_stride * PAGE;
+  EvictArgs a{c->kv + (size_t)first_layer * c->kv_layer_bytes, (int64_t)c->kv_layer_bytes, c->geom, n_layers, n_seq, keep, n_sink,
+              n_recent, row < c->cfg.max_pos ? (int32_t)row : c->cfg.max_pos, d_score, score_stride, d_len, d_page_table,
+              pt_stride, d_new_page_table, new_pt_stride, d_kept, d_score_out, d_new_len};
+  launch_evict(c->bf16, a, (hipStream_t)stream);
+  HIP_TRY(hipGetLastError());
+  return DINFER_OK;
+}
+
+static int check_use(const dinfer_cache_use* use) {
+  if (!use) return fail(DINFER_EINVAL, "use is null");
+  if (use->d_score_in && !use->d_score_out) return fail(DINFER_EINVAL, "d_score_in without d_score_out");
+  if (use->d_score_out && (use->score_stride < 1 || !(use->decay >= 0.f && use->decay < INFINITY)))
+    return fail(DINFER_EINVAL, "score_stride %d, decay %g", use->score_stride, (double)use->decay);
+  return DINFER_OK;
+}
+
+int dinfer_step_scored(dinfer_ctx* c, int32_t n_seq, int32_t block_len, int32_t* d_block_tokens, uint64_t* d_mask,
+                       const int32_t* d_prefix_len, const int32_t* d_page_table, int32_t pt_stride,
+                       const dinfer_decode* decode, const dinfer_cache_use* use, float* d_conf, int32_t* d_argmax,
+                       int32_t* d_n_committed, void* stream) {
+  int rc = check_use(use);
+  if (rc != DINFER_OK) return rc;
+  return step_impl(c, n_seq, block_len, d_block_tokens, d_mask, d_prefix_len, d_page_table, pt_stride, decode, d_conf,
+                   d_argmax, d_n_committed, (hipStream_t)stream, nullptr, nullptr, nullptr, use);
+}
+
+int dinfer_refresh_block_scored(dinfer_ctx* c, int32_t n_seq, int32_t block_len, const int32_t* d_block_tokens,
+                                int32_t* d_prefix_len, const int32_t* d_page_table, int32_t pt_stride,
+                                const dinfer_cache_use* use, void* stream) {
+  int rc = check_block_args(c, n_seq, block_len, d_block_tokens, d_prefix_len, d_page_table, pt_stride);
+  if (rc != DINFER_OK) return rc;
+  if ((rc = check_use(use)) != DINFER_OK) return rc;
+  hipStream_t st = (hipStream_t)stream;
+  rc = forward(c, uniform_span(n_seq, block_len), d_block_tokens, d_prefix_len, d_page_table, pt_stride, false, st, nullptr, use);
+  if (rc != DINFER_OK) return rc;
+  launch_add_i32(d_prefix_len, n_seq, block_len, st);
+  if (use->d_position) launch_add_i32(use->d_position, n_seq, block_len, st);
+  HIP_TRY(hipGetLastError());
+  return DINFER_OK;
 }
 
 int dinfer_stream_read(const void* d_buf, size_t bytes, float* d_sink, void* stream) {

@@ -33,6 +33,7 @@ template <typename E> struct QkvEpi {
   KvGeom geom;
   const int32_t* tok_seq;
   const int32_t* tok_pos;
+  const int32_t* tok_rot;
   const int32_t* page_table;
   int pt_stride;
   const float* cos_tab;
@@ -45,7 +46,7 @@ template <typename E> struct QkvEpi {
   // starts and issues only loads whose addresses are known then; prefetch2() runs behind the stream and issues
   // the loads that depend on the first ones, so that they are under way while the partial sums are folded.
   template <int PER> struct Pre {
-    int pos, seq, page, tok;
+    int pos, rot, seq, page, tok;
     float r;
     float c[PER], s[PER];
   };
@@ -53,6 +54,7 @@ template <typename E> struct QkvEpi {
     Pre<PER> p;
     const int t = valid ? tok : 0;
     p.pos = tok_pos[t];
+    p.rot = tok_rot[t];
     p.seq = tok_seq[t];
     p.tok = t;
     return p;
@@ -64,8 +66,8 @@ template <typename E> struct QkvEpi {
     const int j0 = (task % (hd / 64)) * TILE + acc_row(v0, half);
     const bool rot = task < 2 * geom.n_heads * (hd / 64);
     if constexpr (PER == 4) {   // j0 is a multiple of 4: one 16-byte load per table
-      const f32x4 c4 = *reinterpret_cast<const f32x4*>(cos_tab + (int64_t)p.pos * (hd / 2) + (rot ? j0 : 0));
-      const f32x4 s4 = *reinterpret_cast<const f32x4*>(sin_tab + (int64_t)p.pos * (hd / 2) + (rot ? j0 : 0));
+      const f32x4 c4 = *reinterpret_cast<const f32x4*>(cos_tab + (int64_t)p.rot * (hd / 2) + (rot ? j0 : 0));
+      const f32x4 s4 = *reinterpret_cast<const f32x4*>(sin_tab + (int64_t)p.rot * (hd / 2) + (rot ? j0 : 0));
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         p.c[i] = rot ? c4[i] : 1.f;
@@ -74,8 +76,8 @@ template <typename E> struct QkvEpi {
     } else {
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        p.c[i] = rot ? cos_tab[(int64_t)p.pos * (hd / 2) + j0 + i] : 1.f;
-        p.s[i] = rot ? sin_tab[(int64_t)p.pos * (hd / 2) + j0 + i] : 0.f;
+        p.c[i] = rot ? cos_tab[(int64_t)p.rot * (hd / 2) + j0 + i] : 1.f;
+        p.s[i] = rot ? sin_tab[(int64_t)p.rot * (hd / 2) + j0 + i] : 0.f;
       }
     }
   }
@@ -1081,8 +1083,8 @@ template <typename E, class Epi> static bool configure_dense() {
 
 template <typename E> static void launch_qkv_t(bool bf16, const QkvArgs& a, hipStream_t st) {
   const int D = a.geom.n_heads * a.geom.head_dim;
-  QkvEpi<E> epi{(E*)a.q, a.q_plane, (E*)a.kv_layer, a.geom, a.meta.tok_seq, a.meta.tok_pos, a.page_table,
-                a.pt_stride, a.cos_tab, a.sin_tab, a.norm, a.T, a.H, D};
+  QkvEpi<E> epi{(E*)a.q, a.q_plane, (E*)a.kv_layer, a.geom, a.meta.tok_seq, a.meta.tok_pos, a.meta.tok_rot,
+                a.page_table, a.pt_stride, a.cos_tab, a.sin_tab, a.norm, a.T, a.H, D};
   if (dense_applies(a.T, a.H / ET<E>::KS))
     launch_dense<E>((const E*)a.w, a.H / ET<E>::KS, (const E*)a.xn, a.T, 3 * D / 64, epi, st);
   else if (!single_slice() && half_applies(bf16, a.H, a.T, 3 * D / 64)) {

@@ -34,7 +34,8 @@ void launch_pack_transposed(bool bf16, const void* src, void* dst, int V, int H,
 // ---- forward pieces ----
 struct FwdMeta {            // device arrays describing the tokens of one forward
   const int32_t* tok_seq;   // [T]
-  const int32_t* tok_pos;   // [T] absolute position
+  const int32_t* tok_pos;   // [T] position in the cache
+  const int32_t* tok_rot;   // [T] rotary position: tok_pos, but for a cache that was shortened
   const int32_t* seq_nkeys; // [n_seq] keys visible to the sequence = base + its tokens in this forward
   const int32_t* qtile;     // [n_qtiles][3]: sequence, first packed token, valid rows
 };
@@ -56,6 +57,12 @@ struct RowNorm {
 // The launch also writes the forward's token bookkeeping (FwdMeta's arrays) from `span` and the sequences' first
 // positions d_base (device, or null for 0): `limit` = positions a sequence may use (rotary table and page-table
 // row); a first position that would leave it is pulled back so that no later kernel indexes outside its buffers.
+// rot.first (device, or null): rotary positions of the sequences' first tokens, for rot.tok; kept inside rot.limit alike.
+struct RotaryStart {
+  const int32_t* first;
+  int32_t limit;
+  int32_t* tok;             // [T]
+};
 struct SmoothIn {
   const float* delta;       // [T][H]
   float alpha;
@@ -65,7 +72,7 @@ struct SmoothIn {
 void launch_embed(bool bf16, const int32_t* tokens, const void* emb, int T, int H, int V, float* x,
                   float* ssq, const float* gain, void* xn, const SmoothIn* smooth, const SeqSpan& span,
                   const int32_t* d_base, int limit, int32_t* tok_seq, int32_t* tok_pos, int32_t* seq_nkeys,
-                  int32_t* qtile, hipStream_t st);
+                  int32_t* qtile, const RotaryStart& rot, hipStream_t st);
 // x[t] += sum_j topk_w[t][j] * O[t*k+j];  ssq[t] and xn[t] as above, of the updated row; xn_hi (may be null): LmArgs::xn_hi
 void launch_combine(bool bf16, float* x, const float* O, const float* topk_w, int top_k,
                     int T, int H, float* ssq, const float* gain, void* xn, hipStream_t st, void* xn_hi = nullptr);

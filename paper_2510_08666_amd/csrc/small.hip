@@ -39,8 +39,8 @@ void launch_rope_table(float* cos_tab, float* sin_tab, int max_pos, int head_dim
 // 7.5; now 10.0 and 5.6).
 __device__ inline void token_meta(const SeqSpan& span, const int32_t* __restrict__ d_base, int limit,
                                   int32_t* __restrict__ tok_seq, int32_t* __restrict__ tok_pos,
-                                  int32_t* __restrict__ seq_nkeys, int32_t* __restrict__ qtile) {
-  __shared__ int32_t s_off[MAX_SEQS + 1], s_base[MAX_SEQS], s_tile[MAX_SEQS];
+                                  int32_t* __restrict__ seq_nkeys, int32_t* __restrict__ qtile, const RotaryStart& rot) {
+  __shared__ int32_t s_off[MAX_SEQS + 1], s_base[MAX_SEQS], s_tile[MAX_SEQS], s_rot[MAX_SEQS];
   static_assert(MAX_SEQS <= WAVE, "one lane per sequence");
   const int n_seq = span.n_seq;
   if (threadIdx.x < WAVE) {
@@ -55,6 +55,7 @@ __device__ inline void token_meta(const SeqSpan& span, const int32_t* __restrict
     if ((int)threadIdx.x < n_seq) {
       s_off[s] = o;
       s_base[s] = base;
+      s_rot[s] = rot.first ? max(0, min(rot.first[s], rot.limit - len)) : 0;
       s_tile[s] = incl - tiles;
       seq_nkeys[s] = base + len;
       if (s == n_seq - 1) s_off[n_seq] = o + len;
@@ -70,6 +71,7 @@ __device__ inline void token_meta(const SeqSpan& span, const int32_t* __restrict
     const int at = i - s_off[s];
     tok_seq[i] = s;
     tok_pos[i] = s_base[s] + at;
+    if (rot.first) rot.tok[i] = s_rot[s] + at;
     if (at % TILE == 0) {
       int32_t* q = qtile + (s_tile[s] + at / TILE) * 3;
       q[0] = s;
@@ -105,12 +107,12 @@ __global__ __launch_bounds__(NORM_THREADS) void embed_kernel(const int32_t* __re
                                                              const int32_t* __restrict__ d_base, int limit,
                                                              int32_t* __restrict__ tok_seq, int32_t* __restrict__ tok_pos,
                                                              int32_t* __restrict__ seq_nkeys, int32_t* __restrict__ qtile,
-                                                             const int32_t* __restrict__ live) {
+                                                             RotaryStart rot, const int32_t* __restrict__ live) {
   if (step_is_dead(live)) return;
   __shared__ float sh[4];
   const int t = blockIdx.x;
   if (t == T) {
-    token_meta(span, d_base, limit, tok_seq, tok_pos, seq_nkeys, qtile);
+    token_meta(span, d_base, limit, tok_seq, tok_pos, seq_nkeys, qtile, rot);
     return;
   }
   const E* row = emb + (int64_t)min(max(tokens[t], 0), V - 1) * H;
@@ -137,14 +139,14 @@ __global__ __launch_bounds__(NORM_THREADS) void embed_kernel(const int32_t* __re
 void launch_embed(bool bf16, const int32_t* tokens, const void* emb, int T, int H, int V, float* x,
                   float* ssq, const float* gain, void* xn, const SmoothIn* smooth, const SeqSpan& span,
                   const int32_t* d_base, int limit, int32_t* tok_seq, int32_t* tok_pos, int32_t* seq_nkeys,
-                  int32_t* qtile, hipStream_t st) {
+                  int32_t* qtile, const RotaryStart& rot, hipStream_t st) {
   const SmoothIn sm = smooth ? *smooth : SmoothIn{nullptr, 0.f, nullptr, 1};
   if (bf16)
     embed_kernel<bf16_t><<<T + 1, NORM_THREADS, 0, st>>>(tokens, (const bf16_t*)emb, H, V, x, ssq, gain, (bf16_t*)xn, T, sm,
-                                                         span, d_base, limit, tok_seq, tok_pos, seq_nkeys, qtile, live_word());
+                                                         span, d_base, limit, tok_seq, tok_pos, seq_nkeys, qtile, rot, live_word());
   else
     embed_kernel<float><<<T + 1, NORM_THREADS, 0, st>>>(tokens, (const float*)emb, H, V, x, ssq, gain, (float*)xn, T, sm,
-                                                        span, d_base, limit, tok_seq, tok_pos, seq_nkeys, qtile, live_word());
+                                                        span, d_base, limit, tok_seq, tok_pos, seq_nkeys, qtile, rot, live_word());
 }
 
 // ---------------------------------------------------------------- iteration smoothing: probabilities
