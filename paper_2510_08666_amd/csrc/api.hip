@@ -141,7 +141,7 @@ int attn_splits(int n_qtiles, int n_heads, int key_bound) {
 struct Workspace {
   size_t cos_tab, sin_tab, tok_seq, tok_pos, seq_nkeys, qtile, x, xn, xn_hi, ssq, ssq_a, tk_part, tickets, tickets_bytes, attn_tickets, attn_tickets_bytes, rinv_f, q, a, attn_part, topk_idx, topk_w, cnt, off,
       perm, shares, work, hist, run_tokens, run_base, n_finished, loop_flags, loop_steps, lm_rows, y, o, lm_part, smooth_part, lm_stats, conf, argmax,
-      tok_rot, attend_part, attend_tickets, score_lse, total;
+      tok_rot, attend_part, score_lse, total;
 };
 
 Workspace map_workspace(const dinfer_config& c, int max_seqs, int max_tokens) {
@@ -216,7 +216,6 @@ Workspace map_workspace(const dinfer_config& c, int max_seqs, int max_tokens) {
   w.argmax = cv.take(T * 4);
   w.tok_rot = cv.take(T * 4);                    // rotary positions of a forward over a shortened cache
   w.attend_part = cv.take(attend_part_bytes(c.head_dim));
-  w.attend_tickets = cv.take((size_t)ATTEND_MAX_SHARED * 4);
   w.score_lse = cv.take(T * c.n_heads * 4);      // normalisers of a scored step's rows
   w.total = cv.at;
   return w;
@@ -297,9 +296,8 @@ void score_layer(dinfer_ctx* c, const SeqSpan& span, const int32_t* d_base, int 
   const CacheTokens tok{span, d_base, limit, d_page_table, pt_stride};
   const float scale = 1.f / sqrtf((float)f.head_dim);
   float* lse = at<float>(c->ws, c->wsm.score_lse);
-  AttendArgs aa{tok, {}, kv_layer, c->geom, c->ws + c->wsm.q, D, q_plane, 1, nullptr, scale, nullptr, 0, lse,
-                at<float>(c->ws, c->wsm.attend_part), at<int32_t>(c->ws, c->wsm.attend_tickets)};
-  fill_tiles(span, 1, &aa.tiles);
+  AttendArgs aa{tok, kv_layer, c->geom, c->ws + c->wsm.q, D, q_plane, 1, nullptr, scale, nullptr, 0, lse,
+                at<float>(c->ws, c->wsm.attend_part), false};
   launch_attend(c->bf16, planes, aa, st);
   const int64_t layer_scores = (int64_t)span.n_seq * f.n_heads * use.score_stride * l;
   launch_score(c->bf16, planes,
@@ -530,7 +528,6 @@ int dinfer_create(const dinfer_config* cfg, void* d_weights, size_t weights_byte
   // the arrival counters start at zero and every kernel that uses them leaves them at zero
   if (hipMemsetAsync(c->ws + c->wsm.tickets, 0, c->wsm.tickets_bytes, (hipStream_t)stream) != hipSuccess ||
       hipMemsetAsync(c->ws + c->wsm.attn_tickets, 0, c->wsm.attn_tickets_bytes, (hipStream_t)stream) != hipSuccess ||
-      hipMemsetAsync(c->ws + c->wsm.attend_tickets, 0, (size_t)ATTEND_MAX_SHARED * 4, (hipStream_t)stream) != hipSuccess ||
       hipMemsetAsync(c->ws + c->wsm.off, 0, (size_t)OFF_INTS * 4, (hipStream_t)stream) != hipSuccess) {
     (void)hipHostFree(c->h_mask_pinned);
     delete c;
@@ -1031,6 +1028,10 @@ static int cache_tokens(dinfer_ctx* c, int32_t layer, int32_t n_seq, const int32
       return fail(DINFER_ENOSPACE, "%d new tokens exceed max_pos %d or the page-table row (%d pages)", h_lens[s], c->cfg.max_pos, pt_stride);
     tok->span.off[s + 1] = tok->span.off[s] + h_lens[s];     // <= 64 * 32768
   }
+  // what the kernels number their work by: key tiles of every 32 rows of every cache head
+  const int64_t row_tiles = ((int64_t)tok->span.off[n_seq] * (n_q_heads / c->cfg.n_heads) + TILE - 1) / TILE + n_seq;
+  if (row_tiles * c->cfg.n_heads * ((tok->limit + TILE - 1) / TILE) > INT32_MAX)
+    return fail(DINFER_EUNSUPPORTED, "%d new tokens of %d heads over %d positions are too many for one call", tok->span.off[n_seq], n_q_heads, tok->limit);
   return DINFER_OK;
 }
 static int check_device(const dinfer_ctx* c) {
@@ -1169,7 +1170,6 @@ int dinfer_attend(dinfer_ctx* c, int32_t layer, int32_t n_seq, const int32_t* h_
   if ((rc = check_scale(c, scale, &a.scale)) != DINFER_OK) return rc;
   if ((rc = check_device(c)) != DINFER_OK) return rc;
   a.group = n_q_heads / c->cfg.n_heads;
-  fill_tiles(a.tok.span, a.group, &a.tiles);
   a.kv_layer = c->kv + (size_t)layer * c->kv_layer_bytes;
   a.geom = c->geom;
   a.q = d_q, a.q_stride = q_stride, a.q_plane = 0;
@@ -1177,7 +1177,6 @@ int dinfer_attend(dinfer_ctx* c, int32_t layer, int32_t n_seq, const int32_t* h_
   a.out = d_out, a.out_stride = out_stride;
   a.lse = d_lse;
   a.part = at<float>(c->ws, c->wsm.attend_part);
-  a.tickets = at<int32_t>(c->ws, c->wsm.attend_tickets);
   if (a.tok.span.off[n_seq] == 0) return DINFER_OK;
   launch_attend(c->bf16, 1, a, (hipStream_t)stream);
   HIP_TRY(hipGetLastError());
@@ -1208,9 +1207,8 @@ int dinfer_kv_score(dinfer_ctx* c, int32_t layer, int32_t n_seq, const int32_t* 
   a.score_in = d_score_in, a.score_out = d_score_out, a.score_stride = score_stride;
   if (a.tok.span.off[n_seq] == 0) return DINFER_OK;
   if (!lse_given) {
-    AttendArgs n{a.tok, {}, a.kv_layer, a.geom, d_q, q_stride, 0, a.group, d_visible, a.scale, nullptr, 0, d_lse,
-                 at<float>(c->ws, c->wsm.attend_part), at<int32_t>(c->ws, c->wsm.attend_tickets)};
-    fill_tiles(a.tok.span, a.group, &n.tiles);
+    AttendArgs n{a.tok, a.kv_layer, a.geom, d_q, q_stride, 0, a.group, d_visible, a.scale, nullptr, 0, d_lse,
+                 at<float>(c->ws, c->wsm.attend_part), false};
     launch_attend(c->bf16, 1, n, (hipStream_t)stream);
   }
   launch_score(c->bf16, 1, a, (hipStream_t)stream);

@@ -64,7 +64,6 @@ void launch_append(bool bf16, const AppendArgs& a, hipStream_t st);
 // head * group + r % group.
 struct AttendArgs {
   CacheTokens tok;
-  SeqSpan tiles;              // tiles of 32 rows, per sequence
   const void* kv_layer;
   KvGeom geom;
   const void* q;
@@ -75,14 +74,10 @@ struct AttendArgs {
   void* out;                  // [T] rows of n_heads * group heads, or null: normalisers only
   int64_t out_stride;
   float* lse;                 // [T][n_heads * group] natural logarithm of a row's sum of exponentials, or null
-  float* part;
-  int32_t* tickets;
+  float* part;                // attend_part_bytes
+  bool whole;                 // set by the launch: no pair's keys are cut
 };
-// Workgroups that share (tile, head) pairs' keys never exceed this number, and there are no more pairs than this where
-// keys are shared: what the partial results and the arrival counters are sized by.
-constexpr int ATTEND_MAX_SHARED = 512;
 size_t attend_part_bytes(int head_dim);
-void fill_tiles(const SeqSpan& span, int group, SeqSpan* tiles);
 // planes: of the queries (two: the forward's own bfloat16 queries, normalisers only).
 void launch_attend(bool bf16, int planes, const AttendArgs& a, hipStream_t st);
 
