@@ -341,7 +341,8 @@ int dinfer_rotary_table(const dinfer_rotary* rotary, int32_t max_pos, void* d_ta
 /* Writes the keys and values of new tokens into the cache, and rotates their queries, in one pass:
  *   d_q, d_k, d_v   rows of n_q_heads | n_heads | n_heads heads with strides of their own (parts of one fused matrix are fine).
  *                   d_q may be null: keys and values only.
- *   d_q_gain, d_k_gain [head_dim] float32: RMS norm of every head, x / sqrt(mean(x^2) + eps) * gain, in front of the rotation; null: none.
+ *   d_q_gain, d_k_gain [head_dim] float32, 16-byte aligned: RMS norm of every head, x / sqrt(mean(x^2) + eps) * gain, in front
+ *                   of the rotation; null: none.
  *   rotary, d_table the rotation and its table of table_positions rows (dinfer_rotary_table); rotary null: the
  *                   context's own (whole head, rotate-half, the configuration's theta).
  *   d_positions     [T] rotary positions, null: the cache positions.  Clamped to the table.

@@ -1126,6 +1126,7 @@ int dinfer_kv_append(dinfer_ctx* c, int32_t layer, int32_t n_seq, const int32_t*
     if ((rc = check_rows(c, "d_q_out", d_q_out, q_out_stride, n_q_heads)) != DINFER_OK) return rc;
     if (d_q_out == d_q && q_out_stride != q_stride) return fail(DINFER_EINVAL, "queries in place need one stride");
   }
+  if (((uintptr_t)d_q_gain | (uintptr_t)d_k_gain) & 15) return fail(DINFER_EINVAL, "gains must be 16-byte aligned");
   if ((d_q_gain || d_k_gain) && !(eps >= 0.f && eps < INFINITY)) return fail(DINFER_EINVAL, "eps %g", (double)eps);
   if ((rc = check_device(c)) != DINFER_OK) return rc;
   a.kv_layer = c->kv + (size_t)layer * c->kv_layer_bytes;

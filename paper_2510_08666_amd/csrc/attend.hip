@@ -92,16 +92,6 @@ struct Plan {
   uint32_t end, slot_end, cut_end;     // sums, up to this lane's sequence, of workgroups, partial results, pairs that were cut
   uint32_t total, cut;
 };
-// Sum of v over the lanes up to this one, by lane-to-lane moves inside the registers (rows of 16 lanes, then across them).
-__device__ inline uint32_t lane_scan(uint32_t v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);      // row_shr:1, 2, 4, 8
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // row_bcast:15 into rows 1 and 3
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);      // row_bcast:31 into rows 2 and 3
-  return v;
-}
 template <int ROWS> __device__ inline Plan make_plan(const AttendArgs& a) {
   const int lane = threadIdx.x & 63, s = min(lane, a.tok.span.n_seq - 1);
   const int len = lane == s ? a.tok.span.off[s + 1] - a.tok.span.off[s] : 0;

@@ -31,6 +31,16 @@ __device__ inline int owner_of(const SeqSpan& s, int i) {
   return q;
 }
 
+// Sum of v over the lanes up to this one, by lane-to-lane moves inside the registers (rows of 16 lanes, then across them).
+__device__ inline uint32_t lane_scan(uint32_t v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);      // row_shr:1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);      // row_bcast:15 into rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);      // row_bcast:31 into rows 2 and 3
+  return v;
+}
 // ---- rotary table: rows of rotary_dim / 2 cosines, then (from row max_pos on) as many of sines
 struct RotaryRule {
   int32_t rotary_dim;
