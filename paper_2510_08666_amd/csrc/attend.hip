@@ -16,6 +16,15 @@ namespace dinfer {
 
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 
+static int most_rows(const SeqSpan& span, int group) {
+  int most = 0;
+  for (int s = 0; s < span.n_seq; ++s) {
+    const int rows = (span.off[s + 1] - span.off[s]) * group;
+    most = rows > most ? rows : most;
+  }
+  return most;
+}
+
 // Bit of a key among the sequence's new tokens: keys in front of them are seen by everybody.
 __device__ inline bool sees(uint64_t word, bool masked, int rel) { return rel < 0 || !masked || ((word >> (rel & 63)) & 1); }
 
@@ -46,11 +55,14 @@ template <typename E> __device__ inline u32x4 words_of(const typename ET<E>::vec
 
 // A row's running state takes in one tile of scores: p = exp2(s * c2 - m).  A row that has seen nothing yet keeps m = -inf and
 // p = 0.  The reference maximum moves only when it is passed by more than SLACK (p <= 2^SLACK).
-template <int DT> __device__ inline void take_scores(const f32x16& s, float c2, float& m_run, float& l_run, f32x16 (&o)[DT], float (&p)[16]) {
+template <int DT, int NS>
+__device__ inline void take_scores(const f32x16 (&s)[NS], float c2, float& m_run, float& l_run, f32x16 (&o)[DT], float (&p)[NS][16]) {
   constexpr float SLACK = 6.f;
-  float mx = s[0];
+  float mx = s[0][0];
 #pragma unroll
-  for (int v = 1; v < 16; ++v) mx = fmaxf(mx, s[v]);
+  for (int n = 0; n < NS; ++n)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[n][v]);
   mx = fmaxf(mx, __shfl_xor(mx, 32, WAVE));
   const float mt = mx * c2;
   const bool moves = mt > m_run + SLACK;
@@ -66,10 +78,12 @@ template <int DT> __device__ inline void take_scores(const f32x16& s, float c2, 
   const float ref = m_run > -INFINITY ? m_run : 0.f;
   float sum = 0.f;
 #pragma unroll
-  for (int v = 0; v < 16; ++v) {
-    p[v] = __builtin_amdgcn_exp2f(fmaf(s[v], c2, -ref));
-    sum += p[v];
-  }
+  for (int n = 0; n < NS; ++n)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      p[n][v] = __builtin_amdgcn_exp2f(fmaf(s[n][v], c2, -ref));
+      sum += p[n][v];
+    }
   l_run += sum;
 }
 
@@ -77,34 +91,70 @@ template <int DT> __device__ inline void take_scores(const f32x16& s, float c2, 
 // number (every score NaN: m never moved) makes the sum one.
 __device__ inline float state_weight(float m, float l, float M) { return m > -INFINITY ? __builtin_amdgcn_exp2f(m - M) : l; }
 
+// Indicator of a kind of odd value (0: NaN, 1: +inf, 2: -inf) among the first `valid` elements of an operand.
+template <typename E> __device__ inline typename ET<E>::vec odd_values(const typename ET<E>::vec& x, int kind, int valid) {
+  u32x4 w = words_of<E>(x);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) w[j] &= ValueBits<E>::mask(j, valid);
+  const typename ET<E>::vec y = __builtin_bit_cast(typename ET<E>::vec, w);
+  typename ET<E>::vec is;
+#pragma unroll
+  for (int i = 0; i < ET<E>::G; ++i) {
+    const float f = to_f32(y[i]);
+    is[i] = from_f32<E>((kind == 0 ? f != f : f == (kind == 1 ? INFINITY : -INFINITY)) ? 1.f : 0.f);
+  }
+  return is;
+}
 __device__ inline float log_sum(float m, float l) { return l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * LN2; }
 
 // How a launch deals its work.  A pair is a cache head with a group of ROWS rows of one sequence; the key tiles of a long pair are cut into
 // parts of equal length, a workgroup takes one part, and attend_merge_kernel joins the parts of a pair.  The lengths are on
-// the device, so every wave works the plan out for itself, a lane per sequence.  A part has `per` key tiles at most: as many as leave
-// about ATTEND_PARTS parts, two workgroups on every compute unit, counting half a part per pair for the rounding (a few
-// workgroups more than fit run alone behind the others: 608 of them 39.6 us, 16 sequences of 17 to 32 tokens behind 256 to 2048), and at least MIN_PART
-// (two per wave).  A pair of up to MIN_CUT tiles is left whole: its waves have most of what they need under way at once, and joining
+// the device, so every wave works the plan out for itself, a lane per sequence.  A part has `per` key tiles at most: with few pairs as
+// many as leave about as many parts as workgroups run at a time, counting half a part per pair for the rounding (a few
+// workgroups more than fit run alone behind the others: 16 sequences of 17 to 32 tokens behind 256 to 2048, 608 of them 39.6 us, 496
+// 36.9); with many pairs the compute units' share of all tiles, the longest parts first, so that the short ones fill the gaps; and at least
+// MIN_PART (two per wave).  A pair of up to MIN_CUT tiles is left whole: its waves have most of what they need under way at once, and joining
 // costs more than they take.
-constexpr int ATTEND_PARTS = 512, ATTEND_MIN_CUT = 24, ATTEND_MIN_PART = 8, ATTEND_WAVES = 4;
+constexpr int ATTEND_MIN_CUT = 24, ATTEND_MIN_PART = 8, ATTEND_WAVES = 4;
 struct Plan {
-  int base, tiles, groups, parts;      // of this lane's sequence
-  uint32_t end, slot_end, cut_end;     // sums, up to this lane's sequence, of workgroups, partial results, pairs that were cut
+  int seq, base, tiles, groups, parts;      // of this lane's sequence
+  uint32_t end, slot_end, cut_end;          // sums, up to this lane's sequence, of workgroups, partial results, pairs that were cut
   uint32_t total, cut;
 };
+// Workgroups that run at the same time: two per compute unit, one of those with eight row tiles.
+constexpr int resident(int rows) { return rows > 128 ? 256 : 512; }
 template <int ROWS> __device__ inline Plan make_plan(const AttendArgs& a) {
+  constexpr int PARTS = resident(ROWS);
   const int lane = threadIdx.x & 63, s = min(lane, a.tok.span.n_seq - 1);
   const int len = lane == s ? a.tok.span.off[s + 1] - a.tok.span.off[s] : 0;
   Plan p;
   p.base = cache_base(a.tok, s, len);
   p.tiles = (p.base + len + TILE - 1) / TILE;
   p.groups = (len * a.group + ROWS - 1) / ROWS;
-  const uint32_t pairs = p.groups * a.geom.n_heads;
+  uint32_t pairs = p.groups * a.geom.n_heads;
   const uint32_t units = __builtin_amdgcn_readlane(lane_scan(pairs * p.tiles), WAVE - 1);      // (host: the sum stays below 2^31)
   const uint32_t all_pairs = __builtin_amdgcn_readlane(lane_scan(pairs), WAVE - 1);
-  const uint32_t aim = max((int)(ATTEND_PARTS - all_pairs / 2), ATTEND_PARTS / 2);
+  const bool many = all_pairs > PARTS / 2;
+  const uint32_t aim = many ? PARTS : PARTS - all_pairs / 2;
   const int per = max((int)((units + aim - 1) / aim), ATTEND_MIN_PART);
   p.parts = a.whole || p.tiles <= ATTEND_MIN_CUT ? 1 : (p.tiles + per - 1) / per;
+  p.seq = lane;
+  if (many && a.tok.span.n_seq > 1) {
+    // the longest parts first
+    const int mine = (p.tiles + p.parts - 1) / p.parts;
+    int rank = 0;
+    for (int l = 0; l < a.tok.span.n_seq; ++l) {
+      const int other = __builtin_amdgcn_readlane(mine, l);
+      rank += other > mine || (other == mine && l < lane) ? 1 : 0;
+    }
+    const int to = (lane < a.tok.span.n_seq ? rank : lane) * 4;
+    p.seq = __builtin_amdgcn_ds_permute(to, p.seq);
+    p.base = __builtin_amdgcn_ds_permute(to, p.base);
+    p.tiles = __builtin_amdgcn_ds_permute(to, p.tiles);
+    p.groups = __builtin_amdgcn_ds_permute(to, p.groups);
+    p.parts = __builtin_amdgcn_ds_permute(to, p.parts);
+    pairs = p.groups * a.geom.n_heads;
+  }
   p.end = lane_scan(pairs * p.parts);
   p.cut_end = lane_scan(p.parts > 1 ? pairs : 0);
   p.slot_end = lane_scan(p.parts > 1 ? pairs * p.parts : 0);
@@ -116,39 +166,57 @@ template <int ROWS> __device__ inline Plan make_plan(const AttendArgs& a) {
 struct Piece {
   int seq, base, head, group, part, parts, n_tiles;
   uint32_t slot;      // of the pair's first partial result
+  uint32_t cut;       // its number among the pairs that were cut
 };
-// i: a workgroup's index (below plan.total), or with cut the index of a pair that was cut (below plan.cut).
-__device__ inline Piece piece_at(const Plan& p, uint32_t i, int n_heads, bool cut) {
+// i: a workgroup's index, below plan.total.
+__device__ inline Piece piece_at(const Plan& p, uint32_t i, int n_heads) {
   Piece c;
-  c.seq = __builtin_ctzll(__builtin_amdgcn_ballot_w64((cut ? p.cut_end : p.end) > i));
-  c.base = __builtin_amdgcn_readlane(p.base, c.seq);
-  c.n_tiles = __builtin_amdgcn_readlane(p.tiles, c.seq);
-  c.parts = __builtin_amdgcn_readlane(p.parts, c.seq);
-  const uint32_t groups = __builtin_amdgcn_readlane(p.groups, c.seq), pairs = groups * n_heads;
-  uint32_t pair;
-  if (cut) {
-    pair = i - (__builtin_amdgcn_readlane(p.cut_end, c.seq) - pairs);
-    c.part = 0;
-  } else {
-    const uint32_t at = i - (__builtin_amdgcn_readlane(p.end, c.seq) - pairs * c.parts);
-    pair = at / c.parts;
-    c.part = at % c.parts;
-  }
-  c.slot = __builtin_amdgcn_readlane(p.slot_end, c.seq) - (pairs - pair) * c.parts;
-  c.head = pair / groups;      // (the row groups of a head lie next to each other: they read the same keys)
-  c.group = pair % groups;
+  const int at_lane = __builtin_ctzll(__builtin_amdgcn_ballot_w64(p.end > i));
+  c.seq = __builtin_amdgcn_readlane(p.seq, at_lane);
+  c.base = __builtin_amdgcn_readlane(p.base, at_lane);
+  c.n_tiles = __builtin_amdgcn_readlane(p.tiles, at_lane);
+  c.parts = __builtin_amdgcn_readlane(p.parts, at_lane);
+  const uint32_t groups = __builtin_amdgcn_readlane(p.groups, at_lane), pairs = groups * n_heads;
+  // heads, in them parts, in those row groups: neighbours read the same keys
+  uint32_t at = i - (__builtin_amdgcn_readlane(p.end, at_lane) - pairs * c.parts);
+  c.group = at % groups;
+  at /= groups;
+  c.part = at % c.parts;
+  c.head = at / c.parts;
+  const uint32_t behind = pairs - (c.head * groups + c.group);
+  c.slot = __builtin_amdgcn_readlane(p.slot_end, at_lane) - behind * c.parts;
+  c.cut = __builtin_amdgcn_readlane(p.cut_end, at_lane) - behind;
   return c;
 }
-// What the host sizes grids and partial results by.  Every pair that is cut has more than `per` tiles, per * ATTEND_PARTS covers all
-// tiles: fewer than ATTEND_PARTS pairs are cut, into ceil(tiles / per) < 2 * tiles / per parts each, fewer than
-// 2 * ATTEND_PARTS in all; all workgroups are fewer than ATTEND_PARTS and one more per pair.
-constexpr int ATTEND_SLOTS = 2 * ATTEND_PARTS;
+// What the host sizes grids and partial results by.  Every pair that is cut has more than `per` tiles, and per * resident covers all
+// tiles: fewer than `resident` pairs are cut, into ceil(tiles / per) < 2 * tiles / per parts each, fewer than
+// 2 * resident in all; all workgroups are fewer than `resident` and one more per pair.
+// What the joining kernel is told of a pair that was cut, by the workgroup of its first part: it need not work out the plan again.
+struct alignas(32) CutPair {
+  int32_t seq, row0, head, parts;
+  uint32_t slot, pad[3];
+};
+// In front of the partial results: how many pairs were cut, then their descriptions.
+struct CutList {
+  int32_t n, pad[7];
+  CutPair pair[resident(TILE)];
+};
+__device__ inline void note_cut(const AttendArgs& a, const Plan& plan, const Piece& c, uint32_t wg, int row0) {
+  CutList* list = reinterpret_cast<CutList*>(a.part);
+  if (threadIdx.x != 0) return;
+  if (wg == 0) list->n = plan.cut;
+  if (c.parts > 1 && c.part == 0) list->pair[c.cut] = CutPair{c.seq, row0, c.head, c.parts, c.slot, {}};
+}
+__device__ inline float* attend_part(const AttendArgs& a, uint32_t slot, int floats) {
+  return a.part + sizeof(CutList) / 4 + (int64_t)slot * floats;
+}
 
-// Neighbouring parts run on one die (workgroup i of a launch runs on die i mod 8), all dies have as many, and the workgroups that find
-// nothing to do, since the host can only bound their number, come last.
-__device__ inline uint32_t near_workgroup(uint32_t total) {
-  const uint32_t each = (total + 7) / 8, at = blockIdx.x / 8;
-  return at < each ? blockIdx.x % 8 * each + at : total;
+
+// Workgroup i of a launch runs on die i mod 8: four neighbours run on one die, the next four on the next, and the workgroups that
+// find nothing to do, since the host can only bound their number, come last.  (The launch has a multiple of 32.)
+__device__ inline uint32_t near_workgroup() {
+  const uint32_t i = blockIdx.x, at = i / 8;
+  return at / 4 * 32 + i % 8 * 4 + at % 4;
 }
 
 // RG row tiles per workgroup (RG * 32 rows), each walked by 4 / RG waves that deal its key tiles among them (with two row tiles, both
@@ -175,13 +243,14 @@ __global__ __launch_bounds__(ATTEND_WAVES * WAVE, (attend_waves_per_simd<E, HD>(
   int32_t* pt = reinterpret_cast<int32_t*>(smem + RG * DSTEPS * NP * WAVE * 16);                 // page ids of the piece
   float* lds = reinterpret_cast<float*>(smem);      // behind the key tiles: [ATTEND_WAVES][REGS, then m, l][64 lanes]
   const Plan plan = make_plan<ROWS>(a);
-  const uint32_t wg = near_workgroup(plan.total);
+  const uint32_t wg = near_workgroup();
   if (wg >= plan.total) return;
-  const Piece c = piece_at(plan, wg, a.geom.n_heads, false);
+  const Piece c = piece_at(plan, wg, a.geom.n_heads);
   const int kt0 = c.n_tiles * c.part / c.parts, kt1 = c.n_tiles * (c.part + 1) / c.parts;
   const int tok0 = a.tok.span.off[c.seq], row0 = c.group * ROWS, n_rows = (a.tok.span.off[c.seq + 1] - tok0) * a.group - row0;      // rows from this group on: >= 1
   const int n_keys = c.base + a.tok.span.off[c.seq + 1] - tok0, last_page = (n_keys - 1) / PAGE - 2 * kt0, last_tile = kt1 - 1;
   const int row = row0 + min(rt * TILE + col, n_rows - 1), tok = tok0 + row / a.group, q_head = c.head * a.group + row % a.group;
+  if (!a.whole) note_cut(a, plan, c, wg, row0);
   {
     const int32_t* pages = a.tok.page_table + (int64_t)c.seq * a.tok.pt_stride + 2 * kt0;
     for (int i = threadIdx.x; i <= min(2 * (kt1 - kt0) - 1, last_page); i += ATTEND_WAVES * WAVE) pt[i] = safe_page(a.geom, pages[i]);
@@ -266,12 +335,12 @@ __global__ __launch_bounds__(ATTEND_WAVES * WAVE, (attend_waves_per_simd<E, HD>(
         odd = masked && __builtin_amdgcn_ballot_w64(ValueBits<E>::largest(most) >= ValueBits<E>::ODD) != 0;
       }
     }
-    float p[16];
-    take_scores<DT>(s[0], c2, m_run, l_run, o, p);
+    float p[1][16];
+    take_scores<DT, 1>(s, c2, m_run, l_run, o, p);
     if constexpr (PV) {
       vec pv[STEPS];
 #pragma unroll
-      for (int s2 = 0; s2 < STEPS; ++s2) pv[s2] = PvStep<E>::p_vec(p, s2, 0);
+      for (int s2 = 0; s2 < STEPS; ++s2) pv[s2] = PvStep<E>::p_vec(p[0], s2, 0);
       if (decltype(tail)::value && odd) {
         // 0 * NaN would reach the rows that do not see the key: the product takes 0 in such a value's place, and the rows with
         // weight on it are found by products with its indicator, one kind (NaN, +inf, -inf) at a time, and marked
@@ -296,14 +365,7 @@ __global__ __launch_bounds__(ATTEND_WAVES * WAVE, (attend_waves_per_simd<E, HD>(
 #pragma unroll
             for (int s2 = 0; s2 < STEPS; ++s2) {
               const vec x = PvStep<E>::v_vec(v_row(kt, s2) + t * (TILE * PAGE), half, s2);
-              vec is;
-#pragma unroll
-              for (int i = 0; i < G; ++i) {
-                const float f = to_f32(x[i]);
-                const bool hot = kind == 0 ? f != f : f == (kind == 1 ? INFINITY : -INFINITY);
-                is[i] = from_f32<E>(hot && kt * TILE + PvStep<E>::key_of(s2, half, i) < n_keys ? 1.f : 0.f);
-              }
-              mfma32(hit[0], is, pv[s2]);
+              mfma32(hit[0], odd_values<E>(x, kind, n_keys - (kt * TILE + PvStep<E>::key_of(s2, half, 0))), pv[s2]);
             }
             uint32_t bits = 0;
 #pragma unroll
@@ -377,7 +439,7 @@ __global__ __launch_bounds__(ATTEND_WAVES * WAVE, (attend_waves_per_simd<E, HD>(
     }
   } else {
     constexpr int PROW = PV ? HD : 0;
-    float* part = a.part + (int64_t)(c.slot + c.part) * (ROWS * (PROW + 2));      // [ROWS][HD], then (m, l) [ROWS]
+    float* part = attend_part(a, c.slot + c.part, ROWS * (PROW + 2));      // [ROWS][HD], then (m, l) [ROWS]
 #pragma unroll
     for (int i4 = 0; i4 < OPL / 4; ++i4) {
       const int g = team * OPL + 4 * i4;
@@ -388,56 +450,282 @@ __global__ __launch_bounds__(ATTEND_WAVES * WAVE, (attend_waves_per_simd<E, HD>(
   }
 }
 
+// Many rows (grouped query heads): a workgroup takes WAVES row tiles of a head, one per wave, and every key tile goes through LDS
+// once for all of them, two tiles a turn, double buffered, the turn after next on its way in registers; in the form above
+// each wave would fetch it for itself, and the compute unit's cache bounds the launch (48 sequences of 31 to 64 tokens with four
+// query heads per cache head behind 1000 to 8000: 467 us).  A wave keeps its queries and output in registers, nothing is folded.
+// Bound by the read of K and V, so a workgroup takes up to 256 rows (four waves and 128 rows, two workgroups per compute unit: 300 to
+// 370 us, 1.35 GB fetched).  Of the two waves of a SIMD one has priority, so that it works on its softmax while the other
+// multiplies; in step they would do both one after the other.
+template <int HD> constexpr size_t attend_rows_lds() { return (size_t)2 * 4 * (HD / ET<bf16_t>::KS) * WAVE * 16 + ATTN_MAX_PAGES * 4; }
+template <int HD, int WAVES>
+__global__ __launch_bounds__(WAVES * WAVE, 2) void attend_rows_kernel(AttendArgs a, const int32_t* __restrict__ live) {
+  if (step_is_dead(live)) return;
+  typedef bf16_t E;
+  typedef ET<E>::vec vec;
+  constexpr int G = ET<E>::G, KS = ET<E>::KS, DSTEPS = HD / KS, DT = HD / TILE, STEPS = PvStep<E>::STEPS, ROWS = WAVES * TILE;
+  constexpr int SHARE = WAVES / 4, WF = DSTEPS, MF = WF / SHARE;      // fragments of a set (K or V of one of a turn's two tiles), and those of it that a wave fetches
+  static_assert(DSTEPS == STEPS * DT && STEPS == 2 && (SHARE == 1 || SHARE == 2), "two key tiles have four sets, half a V set is a k-step");
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+  const bool masked = a.visible != nullptr;
+  const E* kv_layer = (const E*)a.kv_layer;
+  extern __shared__ __align__(16) char smem[];
+  auto kv = reinterpret_cast<vec(*)[4][WF][WAVE]>(smem);      // [buffer][K of tile 0, K of tile 1, V of 0, V of 1][fragment][lane]
+  int32_t* pt = reinterpret_cast<int32_t*>(smem + (size_t)2 * 4 * WF * WAVE * 16);
+  __shared__ int32_t odd_turn[2];      // of a buffer: some value of a new token is no finite number
+  const Plan plan = make_plan<ROWS>(a);
+  const uint32_t wg = near_workgroup();
+  if (wg >= plan.total) return;
+  const Piece c = piece_at(plan, wg, a.geom.n_heads);
+  const int kt0 = c.n_tiles * c.part / c.parts, kt1 = c.n_tiles * (c.part + 1) / c.parts;
+  const int tok0 = a.tok.span.off[c.seq], row0 = c.group * ROWS, n_rows = (a.tok.span.off[c.seq + 1] - tok0) * a.group - row0;
+  const int n_keys = c.base + a.tok.span.off[c.seq + 1] - tok0, last_page = (n_keys - 1) / PAGE - 2 * kt0;
+  const int n_turns = (kt1 - kt0 + 1) / 2;
+  const int row = row0 + min(wave * TILE + col, n_rows - 1), tok = tok0 + row / a.group, q_head = c.head * a.group + row % a.group;
+  const bool works = wave * TILE < n_rows;      // (every wave fetches)
+  if (!a.whole) note_cut(a, plan, c, wg, row0);
+  {
+    const int32_t* pages = a.tok.page_table + (int64_t)c.seq * a.tok.pt_stride + 2 * kt0;
+    for (int i = threadIdx.x; i <= min(2 * (kt1 - kt0) - 1, last_page); i += WAVES * WAVE) pt[i] = safe_page(a.geom, pages[i]);
+  }
+  const uint64_t word = masked ? a.visible[tok] : ~0ull;
+  vec q[DSTEPS];
+  {
+    const E* qrow = (const E*)a.q + (int64_t)tok * a.q_stride + q_head * HD + half * G;
+#pragma unroll
+    for (int s = 0; s < DSTEPS; ++s) q[s] = load16<E>(qrow + s * KS);
+  }
+  if (threadIdx.x < 2) odd_turn[threadIdx.x] = 0;
+  __syncthreads();
+  vec next[MF];
+  const int set = wave / SHARE, f0 = wave % SHARE * MF, sub = set & 1;
+  const bool fetch_k = set < 2;
+  const int last_key = min(n_keys, kt1 * TILE) - 1;      // keys past it are another part's, or none
+  auto fetch = [&](int turn) {
+    const int key0 = (kt0 + 2 * min(turn, n_turns - 1) + sub) * TILE;
+    if (fetch_k) {
+      const int key = min(key0 + PvStep<E>::key_of_row(col), last_key);
+      const E* krow = kv_layer + kv_k_index(a.geom, pt[key / PAGE - 2 * kt0], c.head, key % PAGE, 0) + half * G + f0 * (PAGE * KS);
+#pragma unroll
+      for (int j = 0; j < MF; ++j) next[j] = load16<E>(krow + j * (PAGE * KS));
+    } else {
+#pragma unroll
+      for (int h = 0; h < STEPS / SHARE; ++h) {
+        const int step = f0 / DT + h;
+        const int page = pt[min(key0 + PvStep<E>::page_of_step(step) * PAGE, last_key) / PAGE - 2 * kt0];
+        const E* vrow = kv_layer + kv_v_index(a.geom, page, c.head, 0, col);
+#pragma unroll
+        for (int t = 0; t < DT; ++t) next[h * DT + t] = PvStep<E>::v_vec(vrow + t * (TILE * PAGE), half, step);
+      }
+    }
+  };
+  // tail: turns with new tokens or with the end of the part
+  auto put = [&](int turn, auto tail) {
+    const int key0 = (kt0 + 2 * turn + sub) * TILE;
+    if (decltype(tail)::value && !fetch_k) {
+      // new tokens, and the end of the part: values past its last key, which may hold anything, become 0, and so does what is
+      // no finite number where some row may not see it (the rows that do are found below)
+      uint32_t most = 0;
+#pragma unroll
+      for (int h = 0; h < STEPS / SHARE; ++h) {
+        const int valid = last_key + 1 - (key0 + PvStep<E>::key_of(f0 / DT + h, half, 0));
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+          u32x4 w = words_of<E>(next[h * DT + t]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            w[j] &= ValueBits<E>::mask(j, valid);
+            most = ValueBits<E>::larger(most, w[j]);
+            if (masked) w[j] = ValueBits<E>::finite(w[j]);
+          }
+          next[h * DT + t] = __builtin_bit_cast(vec, w);
+        }
+      }
+      if (masked && ValueBits<E>::largest(most) >= ValueBits<E>::ODD) odd_turn[turn & 1] = 1;      // (never taken back: it costs a look)
+    }
+#pragma unroll
+    for (int j = 0; j < MF; ++j) kv[turn & 1][set][f0 + j][lane] = next[j];
+  };
+  f32x16 o[DT];
+  zero_acc<DT>(o);
+  float m_run = -INFINITY, l_run = 0.f;
+  uint64_t marks[3] = {0, 0, 0};
+  const float c2 = a.scale * LOG2E;
+  auto take_turn = [&](int turn, auto tail) {
+    const auto& tiles = kv[turn & 1];
+    // LDS fragments are read RD ahead of the matrix instructions that take them, behind the last ones of K the first of V
+    // (pinned by the scheduling barriers: all at once they would take the registers of the queries)
+    constexpr int RD = 4, NF = 2 * DSTEPS;
+    vec ring[RD];
+    f32x16 s[2];
+    zero_acc<2>(s);
+#pragma unroll
+    for (int f = 0; f < RD; ++f) ring[f] = tiles[f & 1][f >> 1][lane];
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {      // k-step f / 2 of tile f % 2
+      const vec k = ring[f % RD];
+      const int n = f + RD;
+      ring[f % RD] = n < NF ? tiles[n & 1][n >> 1][lane] : tiles[2][n - NF][lane];
+      __builtin_amdgcn_sched_barrier(0);
+      mfma32(s[f & 1], k, q[f / 2]);
+    }
+    const int first_key = (kt0 + 2 * turn) * TILE;
+    bool odd = false;
+    if constexpr (decltype(tail)::value) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int key = first_key + n * TILE + PvStep<E>::key_of_acc(v, half);
+          if (key > last_key || !sees(word, masked, key - c.base)) s[n][v] = -INFINITY;
+        }
+      odd = odd_turn[turn & 1] != 0;
+    }
+    float p[2][16];
+    take_scores<DT, 2>(s, c2, m_run, l_run, o, p);
+    if (decltype(tail)::value && odd) {
+      // see attend_kernel: rows with weight on a value that is no finite number are marked
+#pragma unroll 1
+      for (int t = 0; t < DT; ++t)
+#pragma unroll 1
+        for (int kind = 0; kind < 3; ++kind) {
+          f32x16 hit[1];
+          zero_acc<1>(hit);
+#pragma unroll
+          for (int u = 0; u < 2 * STEPS; ++u) {
+            const int key0 = first_key + u / STEPS * TILE;
+            const int page = pt[min(key0 + PvStep<E>::page_of_step(u % STEPS) * PAGE, last_key) / PAGE - 2 * kt0];
+            const vec x = PvStep<E>::v_vec(kv_layer + kv_v_index(a.geom, page, c.head, 0, t * TILE + col), half, u % STEPS);
+            mfma32(hit[0], odd_values<E>(x, kind, last_key + 1 - (key0 + PvStep<E>::key_of(u % STEPS, half, 0))), PvStep<E>::p_vec(p[u / STEPS], u % STEPS, 0));
+          }
+          uint32_t bits = 0;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) bits |= hit[0][i] != 0.f ? 1u << i : 0u;
+          marks[kind] |= (uint64_t)bits << (16 * t);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < 2 * STEPS; ++u) {
+      const vec pv = PvStep<E>::p_vec(p[u / STEPS], u % STEPS, 0);
+#pragma unroll
+      for (int t = 0; t < DT; ++t) {
+        const int f = u * DT + t;
+        const vec v = ring[f % RD];
+        if (f + RD < NF) ring[f % RD] = tiles[2 + (f + RD) / WF][(f + RD) % WF][lane];
+        __builtin_amdgcn_sched_barrier(0);
+        mfma32(o[t], v, pv);
+      }
+    }
+  };
+  // The turns in front of the tail, and the one before it, whose neighbour has to be masked on its way to LDS.
+  const int full = (min(c.base, last_key + 1) - kt0 * TILE) / (2 * TILE);
+  if (SHARE == 2 && wave < 4) __builtin_amdgcn_s_setprio(1);
+  fetch(0);
+  put(0, std::true_type{});
+  fetch(1);
+  int turn = 0;
+  for (; turn + 1 < full; ++turn) {
+    __syncthreads();      // this turn's tiles are in their buffer, and every wave has done with the other one
+    put(turn + 1, std::false_type{});
+    fetch(turn + 2);
+    if (works) take_turn(turn, std::false_type{});
+  }
+  for (; turn < n_turns; ++turn) {
+    __syncthreads();
+    if (turn + 1 < n_turns) {
+      put(turn + 1, std::true_type{});
+      fetch(turn + 2);
+    }
+    if (works) take_turn(turn, std::true_type{});
+  }
+  if (wave * TILE + col >= n_rows) return;
+  if (__builtin_amdgcn_ballot_w64((marks[0] | marks[1] | marks[2]) != 0)) {
+#pragma unroll
+    for (int i = 0; i < DT * 16; ++i) {
+      if ((marks[1] >> i) & 1) o[i / 16][i % 16] += INFINITY;
+      if ((marks[2] >> i) & 1) o[i / 16][i % 16] -= INFINITY;
+      if ((marks[0] >> i) & 1) o[i / 16][i % 16] = __builtin_nanf("");
+    }
+  }
+  const float L = l_run + __shfl_xor(l_run, 32, WAVE);
+  if (c.parts == 1) {
+    if (a.lse && half == 0) a.lse[(int64_t)tok * (a.geom.n_heads * a.group) + q_head] = log_sum(m_run, L);
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        store_elems4<E>((E*)a.out + (int64_t)tok * a.out_stride + q_head * HD + t * TILE + acc_row(4 * g, half),
+                        f32x4{o[t][4 * g] * inv, o[t][4 * g + 1] * inv, o[t][4 * g + 2] * inv, o[t][4 * g + 3] * inv});
+  } else {
+    float* part = attend_part(a, c.slot + c.part, ROWS * (HD + 2));
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4*>(part + (wave * TILE + col) * HD + t * TILE + acc_row(4 * g, half)) =
+            f32x4{o[t][4 * g], o[t][4 * g + 1], o[t][4 * g + 2], o[t][4 * g + 3]};
+    if (half == 0) *reinterpret_cast<float2*>(part + ROWS * HD + 2 * (wave * TILE + col)) = float2{m_run, L};
+  }
+}
+
 // Joins the parts of the pairs that were cut, in key order, each weighted against the maximum of all.  A thread takes four consecutive
-// features of a row; a workgroup's rows belong to one pair.  Bound by the read of the partial results.
+// features of a row; a workgroup's rows belong to one pair.  Bound by the latency of its two loads (the pair, its partial
+// results), and by the read of these.
 constexpr int MERGE_THREADS = 256;
+template <int HD, bool PV> constexpr int merge_rows() { return PV ? MERGE_THREADS / (HD / 4) : 32; }      // rows of a pass
 template <typename E, int HD, int ROWS, bool PV>
 __global__ __launch_bounds__(MERGE_THREADS) void attend_merge_kernel(AttendArgs a, const int32_t* __restrict__ live) {
   if (step_is_dead(live)) return;
-  constexpr int CHUNKS = PV ? HD / 4 : 1, PROW = PV ? HD : 0, PER = MERGE_THREADS / CHUNKS < ROWS ? MERGE_THREADS / CHUNKS : ROWS;
-  const Plan plan = make_plan<ROWS>(a);
-  const int q = blockIdx.x % (ROWS / PER) * PER + (int)threadIdx.x / CHUNKS, d = threadIdx.x % CHUNKS * 4;
-  const uint32_t pair = blockIdx.x / (ROWS / PER);
-  if (pair >= plan.cut) return;
-  const Piece c = piece_at(plan, pair, a.geom.n_heads, true);
-  const int row = c.group * ROWS + q, n_rows = (a.tok.span.off[c.seq + 1] - a.tok.span.off[c.seq]) * a.group;
-  if ((int)threadIdx.x / CHUNKS >= PER || row >= n_rows) return;
-  const float* part = a.part + (int64_t)c.slot * (ROWS * (PROW + 2));
-  float M = -INFINITY, L = 0.f;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  constexpr int N = 8;      // parts whose loads are under way together
-  for (int p0 = 0; p0 < c.parts; p0 += N) {
-    float2 ml[N];
-    f32x4 o[N];
+  constexpr int CHUNKS = PV ? HD / 4 : 1, PROW = PV ? HD : 0, PER = merge_rows<HD, PV>(), PASSES = ROWS > 64 ? 4 : 1;
+  constexpr int WGS = ROWS / (PER * PASSES);      // workgroups of a pair
+  static_assert(WGS * PER * PASSES == ROWS, "whole passes");
+  const CutList* list = reinterpret_cast<const CutList*>(a.part);
+  const int pair = blockIdx.x / WGS, n = list->n;
+  const CutPair c = list->pair[pair];
+  if (pair >= n) return;
+  const int n_rows = (a.tok.span.off[c.seq + 1] - a.tok.span.off[c.seq]) * a.group;
+  if ((int)threadIdx.x / CHUNKS >= PER) return;
+  for (int pass = 0; pass < PASSES; ++pass) {
+    const int q = (blockIdx.x % WGS * PASSES + pass) * PER + (int)threadIdx.x / CHUNKS, d = threadIdx.x % CHUNKS * 4, row = c.row0 + q;
+    if (row >= n_rows) return;
+    const float* part = attend_part(a, c.slot, ROWS * (PROW + 2));
+    float M = -INFINITY, L = 0.f;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    constexpr int N = 8;      // parts whose loads are under way together
+    for (int p0 = 0; p0 < c.parts; p0 += N) {
+      float2 ml[N];
+      f32x4 o[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float* from = part + (int64_t)min(p0 + i, c.parts - 1) * (ROWS * (PROW + 2));
-      ml[i] = *reinterpret_cast<const float2*>(from + ROWS * PROW + 2 * q);
-      if constexpr (PV) o[i] = *reinterpret_cast<const f32x4*>(from + q * PROW + d);
-    }
-    float top = M;
+      for (int i = 0; i < N; ++i) {
+        const float* from = part + (int64_t)min(p0 + i, c.parts - 1) * (ROWS * (PROW + 2));
+        ml[i] = *reinterpret_cast<const float2*>(from + ROWS * PROW + 2 * q);
+        if constexpr (PV) o[i] = *reinterpret_cast<const f32x4*>(from + q * PROW + d);
+      }
+      float top = M;
 #pragma unroll
-    for (int i = 0; i < N; ++i) top = fmaxf(top, ml[i].x);
-    const float old = M > -INFINITY ? __builtin_amdgcn_exp2f(M - top) : 1.f;      // (nothing so far: L and acc are 0, or NaN)
-    L *= old;
-    if constexpr (PV) acc *= old;
+      for (int i = 0; i < N; ++i) top = fmaxf(top, ml[i].x);
+      const float old = M > -INFINITY ? __builtin_amdgcn_exp2f(M - top) : 1.f;      // (nothing so far: L and acc are 0, or NaN)
+      L *= old;
+      if constexpr (PV) acc *= old;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      if (p0 + i < c.parts) {
-        const float w = state_weight(ml[i].x, ml[i].y, top);
-        L = fmaf(w, ml[i].y, L);
-        if constexpr (PV) {
+      for (int i = 0; i < N; ++i) {
+        if (p0 + i < c.parts) {
+          const float w = state_weight(ml[i].x, ml[i].y, top);
+          L = fmaf(w, ml[i].y, L);
+          if constexpr (PV) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) acc[k] = fmaf(w, o[i][k], acc[k]);
+            for (int k = 0; k < 4; ++k) acc[k] = fmaf(w, o[i][k], acc[k]);
+          }
         }
       }
+      M = top;
     }
-    M = top;
+    const int64_t tok = a.tok.span.off[c.seq] + row / a.group;
+    const int q_head = c.head * a.group + row % a.group;
+    if (a.lse && d == 0) a.lse[tok * (a.geom.n_heads * a.group) + q_head] = log_sum(M, L);
+    if constexpr (PV) store_elems4<E>((E*)a.out + tok * a.out_stride + q_head * HD + d, acc * (L == 0.f ? 0.f : 1.f / L));
   }
-  const int64_t tok = a.tok.span.off[c.seq] + row / a.group;
-  const int q_head = c.head * a.group + row % a.group;
-  if (a.lse && d == 0) a.lse[tok * (a.geom.n_heads * a.group) + q_head] = log_sum(M, L);
-  if constexpr (PV) store_elems4<E>((E*)a.out + tok * a.out_stride + q_head * HD + d, acc * (L == 0.f ? 0.f : 1.f / L));
 }
 
 template <typename E, int HD, int NP, int RG, bool PV> constexpr size_t attend_lds() {
@@ -445,34 +733,49 @@ template <typename E, int HD, int NP, int RG, bool PV> constexpr size_t attend_l
   const size_t walk = (size_t)RG * (HD / ET<E>::KS) * NP * WAVE * 16 + ATTN_MAX_PAGES * 4;
   return fold > walk ? fold : walk;
 }
-size_t attend_part_bytes(int head_dim) { return (size_t)ATTEND_SLOTS * 2 * TILE * (head_dim + 2) * 4; }
+size_t attend_part_bytes(int head_dim, int max_pos) {
+  if (max_pos <= ATTEND_MIN_CUT * TILE) return 0;      // nothing is cut
+  const size_t rows = (size_t)2 * resident(8 * TILE) * 8 * TILE, few = (size_t)2 * resident(4 * TILE) * 4 * TILE;
+  return (rows > few ? rows : few) * (head_dim + 2) * 4 + sizeof(CutList);
+}
 
-template <typename E, int HD, int NP, int RG, bool PV> static void launch_attend_t(AttendArgs a, hipStream_t st) {
-  constexpr int ROWS = RG * TILE, PER = MERGE_THREADS / (PV ? HD / 4 : 1) < ROWS ? MERGE_THREADS / (PV ? HD / 4 : 1) : ROWS;
+// Grids: workgroups of the first launch, pairs that may have to be joined (none: a.whole).
+struct AttendGrid {
+  unsigned wgs, cut;
+};
+template <int ROWS> static AttendGrid attend_grid(AttendArgs& a) {
   int64_t pairs = 0;
   for (int s = 0; s < a.tok.span.n_seq; ++s) pairs += ((int64_t)(a.tok.span.off[s + 1] - a.tok.span.off[s]) * a.group + ROWS - 1) / ROWS;
   pairs *= a.geom.n_heads;
   a.whole = single_slice() || a.tok.limit <= ATTEND_MIN_CUT * TILE;
-  const int64_t wgs = a.whole ? pairs : pairs + ATTEND_PARTS;
-  attend_kernel<E, HD, NP, RG, PV><<<(unsigned)((wgs + 7) / 8 * 8), ATTEND_WAVES * WAVE, attend_lds<E, HD, NP, RG, PV>(), st>>>(a, live_word());
-  if (a.whole) return;
-  const int64_t cut = pairs < ATTEND_PARTS ? pairs : ATTEND_PARTS;
-  attend_merge_kernel<E, HD, ROWS, PV><<<(unsigned)(cut * (ROWS / PER)), MERGE_THREADS, 0, st>>>(a, live_word());
+  const int64_t wgs = a.whole ? pairs : pairs + resident(ROWS);
+  return AttendGrid{(unsigned)((wgs + 31) / 32 * 32), a.whole ? 0u : (unsigned)(pairs < resident(ROWS) ? pairs : resident(ROWS))};
+}
+template <typename E, int HD, int ROWS, bool PV> static void launch_merge(const AttendArgs& a, unsigned cut, hipStream_t st) {
+  if (cut > 0) attend_merge_kernel<E, HD, ROWS, PV><<<cut * (ROWS / (merge_rows<HD, PV>() * (ROWS > 64 ? 4 : 1))), MERGE_THREADS, 0, st>>>(a, live_word());
+}
+template <typename E, int HD, int NP, int RG, bool PV> static void launch_attend_t(AttendArgs a, hipStream_t st) {
+  const AttendGrid g = attend_grid<RG * TILE>(a);
+  attend_kernel<E, HD, NP, RG, PV><<<g.wgs, ATTEND_WAVES * WAVE, attend_lds<E, HD, NP, RG, PV>(), st>>>(a, live_word());
+  launch_merge<E, HD, RG * TILE, PV>(a, g.cut, st);
+}
+template <int HD, int WAVES> static void launch_attend_rows(AttendArgs a, hipStream_t st) {
+  const AttendGrid g = attend_grid<WAVES * TILE>(a);
+  attend_rows_kernel<HD, WAVES><<<g.wgs, WAVES * WAVE, attend_rows_lds<HD>(), st>>>(a, live_word());
+  launch_merge<bf16_t, HD, WAVES * TILE, true>(a, g.cut, st);
 }
 template <typename E, int HD, int RG> static void launch_attend_rg(int planes, const AttendArgs& a, hipStream_t st) {
   if (a.out) launch_attend_t<E, HD, 1, RG, true>(a, st);
   else if (planes == 1) launch_attend_t<E, HD, 1, RG, false>(a, st);
   else if constexpr (sizeof(E) == 2) launch_attend_t<E, HD, 2, RG, false>(a, st);
 }
-// Two row tiles per workgroup where a sequence has more than one.
+// Two row tiles per workgroup where a sequence has more than one; more than two: the form whose tiles go through LDS (bfloat16).
 template <int HD> static void launch_attend_hd(bool bf16, int planes, const AttendArgs& a, hipStream_t st) {
-  int most = 0;
-  for (int s = 0; s < a.tok.span.n_seq; ++s) {
-    const int rows = (a.tok.span.off[s + 1] - a.tok.span.off[s]) * a.group;
-    most = rows > most ? rows : most;
-  }
+  const int most = most_rows(a.tok.span, a.group);
   if (bf16) {
-    if (most <= TILE) launch_attend_rg<bf16_t, HD, 1>(planes, a, st);
+    if (most > 4 * TILE && a.out) launch_attend_rows<HD, 8>(a, st);
+    else if (most > 2 * TILE && a.out) launch_attend_rows<HD, 4>(a, st);
+    else if (most <= TILE) launch_attend_rg<bf16_t, HD, 1>(planes, a, st);
     else launch_attend_rg<bf16_t, HD, 2>(planes, a, st);
   } else {
     if (most <= TILE) launch_attend_rg<float, HD, 1>(planes, a, st);
@@ -488,10 +791,14 @@ template <typename E, int HD, int RG> static bool configure_attend_t() {
   return hipFuncSetAttribute((const void*)attend_kernel<E, HD, 1, RG, true>, hipFuncAttributeMaxDynamicSharedMemorySize,
                              (int)attend_lds<E, HD, 1, RG, true>()) == hipSuccess;
 }
+template <int HD, int WAVES> static bool configure_rows() {
+  return hipFuncSetAttribute((const void*)attend_rows_kernel<HD, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)attend_rows_lds<HD>()) == hipSuccess;
+}
 bool configure_attend() {
   const bool ok = configure_attend_t<bf16_t, 128, 1>() && configure_attend_t<bf16_t, 128, 2>() && configure_attend_t<bf16_t, 64, 1>() &&
                   configure_attend_t<bf16_t, 64, 2>() && configure_attend_t<float, 128, 1>() && configure_attend_t<float, 128, 2>() &&
-                  configure_attend_t<float, 64, 1>() && configure_attend_t<float, 64, 2>();
+                  configure_attend_t<float, 64, 1>() && configure_attend_t<float, 64, 2>() && configure_rows<128, 4>() &&
+                  configure_rows<128, 8>() && configure_rows<64, 4>() && configure_rows<64, 8>();
   (void)hipGetLastError();
   return ok;
 }
@@ -500,75 +807,105 @@ bool configure_attend() {
 // Attention weight that cached positions gather: score[head][key] = decay * score[head][key] + the sum over the rows of the
 // head's group of exp(scale * q . k - lse).  Here rows run along the registers and keys along the lanes (A = Q, B = K), so a
 // key's sum over 32 rows is an addition of 16 registers and one exchange between the half-waves, and every score has one writer:
-// no atomics, the same bits every time.  Bound by the read of K.
+// no atomics, the same bits every time.  A wave holds KT key tiles in registers, all their loads under way at once, and meets them with
+// one row tile after the other.  Bound by the read of K; with many rows by the matrix instructions and the queries' second
+// reads, which KT tiles share (16 KB of keys per wave: what fits the registers beside the queries).
 // ------------------------------------------------------------------------------------------------
 constexpr int SCORE_WAVES = 4;
+template <typename E, int HD> constexpr int score_tiles() { return 512 / (sizeof(E) * HD); }
 template <typename E, int HD, int NP>
-__global__ __launch_bounds__(SCORE_WAVES * WAVE) void score_kernel(ScoreArgs a, const int32_t* __restrict__ live) {
+__global__ __launch_bounds__(SCORE_WAVES * WAVE, 2) void score_kernel(ScoreArgs a, const int32_t* __restrict__ live) {
   if (step_is_dead(live)) return;
   typedef typename ET<E>::vec vec;
-  constexpr int G = ET<E>::G, KS = ET<E>::KS, DSTEPS = HD / KS;
+  constexpr int G = ET<E>::G, KS = ET<E>::KS, DSTEPS = HD / KS, KT = score_tiles<E, HD>();
   const int head = blockIdx.y, seq = blockIdx.z;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
   const int tok0 = a.tok.span.off[seq], len = a.tok.span.off[seq + 1] - tok0;
   if (len == 0) return;
   const int base = cache_base(a.tok, seq, len), n_keys = min(base + len, a.score_stride);
-  const int kt = blockIdx.x * SCORE_WAVES + wave, n_rows = len * a.group;
-  if (kt * TILE >= n_keys) return;
+  const int kt0 = (blockIdx.x * SCORE_WAVES + wave) * KT, n_rows = len * a.group;
+  if (kt0 * TILE >= n_keys) return;
   const bool masked = a.visible != nullptr;
-  const int key = kt * TILE + col, n_q_heads = a.geom.n_heads * a.group;
-  vec k[DSTEPS];
-  {
-    const int at = min(key, n_keys - 1);
-    const int page = safe_page(a.geom, a.tok.page_table[(int64_t)seq * a.tok.pt_stride + at / PAGE]);
-    const E* krow = (const E*)a.kv_layer + kv_k_index(a.geom, page, head, at % PAGE, 0) + half * G;
+  const int n_q_heads = a.geom.n_heads * a.group;
+  const int32_t* pages = a.tok.page_table + (int64_t)seq * a.tok.pt_stride;
+  int page[KT];
 #pragma unroll
-    for (int s = 0; s < DSTEPS; ++s) k[s] = load16<E>(krow + s * (PAGE * KS));
+  for (int i = 0; i < KT; ++i) page[i] = pages[min((kt0 + i) * TILE + col, n_keys - 1) / PAGE];
+  auto row_at = [&](int row0) { return row0 + min(col, n_rows - row0 - 1); };
+  auto load_q = [&](int row0, vec (&q)[DSTEPS * NP], float& lse, uint64_t& word) {
+    const int row = row_at(row0), tok = tok0 + row / a.group, q_head = head * a.group + row % a.group;
+    const E* qrow = (const E*)a.q + (int64_t)tok * a.q_stride + q_head * HD + half * G;
+#pragma unroll
+    for (int i = 0; i < DSTEPS * NP; ++i) q[i] = load16<E>(qrow + (i % NP) * a.q_plane + (i / NP) * KS);
+    lse = a.lse[(int64_t)tok * n_q_heads + q_head];
+    word = masked ? a.visible[tok] : ~0ull;
+  };
+  vec q[DSTEPS * NP], k[KT][DSTEPS];
+  float lse;
+  uint64_t word;
+  load_q(0, q, lse, word);
+#pragma unroll
+  for (int i = 0; i < KT; ++i) {
+    const int at = min((kt0 + i) * TILE + col, n_keys - 1);
+    const E* krow = (const E*)a.kv_layer + kv_k_index(a.geom, safe_page(a.geom, page[i]), head, at % PAGE, 0) + half * G;
+#pragma unroll
+    for (int s = 0; s < DSTEPS; ++s) k[i][s] = load16<E>(krow + s * (PAGE * KS));
   }
-  __shared__ float s_lse[SCORE_WAVES][TILE];
+  __shared__ __align__(16) float s_lse[SCORE_WAVES][TILE];
   __shared__ uint64_t s_word[SCORE_WAVES][TILE];
   const float c2 = a.scale * LOG2E;
-  float sum = 0.f;
-  for (int row0 = 0; row0 < n_rows; row0 += TILE) {
-    const int row = row0 + min(col, n_rows - row0 - 1), tok = tok0 + row / a.group, q_head = head * a.group + row % a.group;
-    const E* qrow = (const E*)a.q + (int64_t)tok * a.q_stride + q_head * HD + half * G;
-    f32x16 s[1];
-    zero_acc<1>(s);
+  const bool tail = masked && (kt0 + KT) * TILE > base;
+  float sum[KT];
 #pragma unroll
-    for (int i = 0; i < DSTEPS * NP; ++i) mfma32(s[0], load16<E>(qrow + (i % NP) * a.q_plane + (i / NP) * KS), k[i / NP]);
+  for (int i = 0; i < KT; ++i) sum[i] = 0.f;
+  for (int row0 = 0; row0 < n_rows; row0 += TILE) {
     if (half == 0) {
-      // rows past the last one, and rows that see nothing (lse = -inf), weigh nothing
-      const float lse = a.lse[(int64_t)tok * n_q_heads + q_head];
+      // rows past the last one, and rows that see nothing (lse = -inf), weigh nothing: exp2(x - inf) = 0
       s_lse[wave][col] = row0 + col < n_rows && lse != -INFINITY ? lse * LOG2E : INFINITY;
-      s_word[wave][col] = masked ? a.visible[tok] : ~0ull;
+      s_word[wave][col] = word;
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    const bool tail = (kt + 1) * TILE > base && masked;
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      const float l = s_lse[wave][acc_row(v, half)];
-      float p = __builtin_amdgcn_exp2f(fmaf(s[0][v], c2, -l));
-      if (l == INFINITY) p = 0.f;                                             // (a score that is not a number included)
-      if (tail && !sees(s_word[wave][acc_row(v, half)], true, key - base)) p = 0.f;
-      sum += p;
+    for (int i = 0; i < KT; ++i) {
+      f32x16 s[1];
+      zero_acc<1>(s);
+#pragma unroll
+      for (int f = 0; f < DSTEPS * NP; ++f) mfma32(s[0], q[f], k[i][f / NP]);
+      const int rel = (kt0 + i) * TILE + col - base;
+#pragma unroll
+      for (int v4 = 0; v4 < 4; ++v4) {
+        const f32x4 l4 = *reinterpret_cast<const f32x4*>(&s_lse[wave][acc_row(4 * v4, half)]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float p = __builtin_amdgcn_exp2f(fmaf(s[0][4 * v4 + j], c2, -l4[j]));
+          if (l4[j] == INFINITY) p = 0.f;                                      // (a score that is no number included)
+          if (tail && !sees(s_word[wave][acc_row(4 * v4 + j, half)], true, rel)) p = 0.f;
+          sum[i] += p;
+        }
+      }
     }
+    if (row0 + TILE < n_rows) load_q(row0 + TILE, q, lse, word);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }
-  sum += __shfl_xor(sum, 32, WAVE);
-  if (half == 0 && key < n_keys) {
-    const int64_t at = ((int64_t)seq * a.geom.n_heads + head) * a.score_stride + key;
-    a.score_out[at] = a.score_in ? fmaf(a.decay, a.score_in[at], sum) : sum;
+  const int64_t unit = ((int64_t)seq * a.geom.n_heads + head) * a.score_stride;
+#pragma unroll
+  for (int i = 0; i < KT; ++i) {
+    const float total = sum[i] + __shfl_xor(sum[i], 32, WAVE);
+    const int key = (kt0 + i) * TILE + col;
+    if (half == 0 && key < n_keys) a.score_out[unit + key] = a.score_in ? fmaf(a.decay, a.score_in[unit + key], total) : total;
   }
 }
 
+template <typename E, int HD, int NP> static void launch_score_t(const ScoreArgs& a, hipStream_t st) {
+  const int bound = a.tok.limit < a.score_stride ? a.tok.limit : a.score_stride, keys = SCORE_WAVES * score_tiles<E, HD>() * TILE;
+  score_kernel<E, HD, NP><<<dim3((bound + keys - 1) / keys, a.geom.n_heads, a.tok.span.n_seq), SCORE_WAVES * WAVE, 0, st>>>(a, live_word());
+}
 template <int HD> static void launch_score_hd(bool bf16, int planes, const ScoreArgs& a, hipStream_t st) {
-  const int bound = a.tok.limit < a.score_stride ? a.tok.limit : a.score_stride;
-  const dim3 grid((bound + SCORE_WAVES * TILE - 1) / (SCORE_WAVES * TILE), a.geom.n_heads, a.tok.span.n_seq);
-  if (!bf16) score_kernel<float, HD, 1><<<grid, SCORE_WAVES * WAVE, 0, st>>>(a, live_word());
-  else if (planes == 1) score_kernel<bf16_t, HD, 1><<<grid, SCORE_WAVES * WAVE, 0, st>>>(a, live_word());
-  else score_kernel<bf16_t, HD, 2><<<grid, SCORE_WAVES * WAVE, 0, st>>>(a, live_word());
+  if (!bf16) launch_score_t<float, HD, 1>(a, st);
+  else if (planes == 1) launch_score_t<bf16_t, HD, 1>(a, st);
+  else launch_score_t<bf16_t, HD, 2>(a, st);
 }
 void launch_score(bool bf16, int planes, const ScoreArgs& a, hipStream_t st) {
   if (a.geom.head_dim == 128) launch_score_hd<128>(bf16, planes, a, st);

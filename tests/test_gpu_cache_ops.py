@@ -143,8 +143,9 @@ def test_append_like_the_step(m):
 
 # ------------------------------------------------------------------------------------------------ attend
 
+# (past 4001 and more: keys cut into parts; many sequences: the longest parts first)
 LENS = [([1, 0, 33, 64, 7], [0, 5, 16, 500, 31]), ([1], [0]), ([1], [2000]), ([64], [8000]), ([2, 5, 31], [0, 0, 1]),
-        ([20, 32, 1, 3, 64, 40], [800, 31, 1600, 0, 4001, 768])]
+        ([20, 32, 1, 3, 64, 40], [800, 31, 1600, 0, 4001, 768]), ([3, 0, 7, 64] * 12, [40 * i for i in range(48)])]
 
 
 @pytest.mark.parametrize("dtype,heads,hd", SHAPES)
@@ -191,8 +192,10 @@ def test_attend_long_runs_without_words(m):
 
 @pytest.mark.parametrize("dtype,heads,hd", SHAPES)
 @pytest.mark.parametrize("past", [0, 37, 900])
-def test_attend_what_is_hidden_does_not_reach(m, dtype, heads, hd, past):
-    """NaN and infinities in new keys and values that a token does not see, and behind the last key; those it sees do reach it."""
+@pytest.mark.parametrize("group", [1, 2, 3, 9])
+def test_attend_what_is_hidden_does_not_reach(m, dtype, heads, hd, past, group):
+    """NaN and infinities in new keys and values that a token does not see, and behind the last key; those it sees do reach it.
+    (The groups choose the forms: 30, 60, 90 and 270 rows per cache head.)"""
     torch = m.torch
     n = 30
     c = m.Cache(dtype, heads, hd, [n, 9], [past, 3], seed=7)
@@ -200,31 +203,38 @@ def test_attend_what_is_hidden_does_not_reach(m, dtype, heads, hd, past):
     kv = torch.randn(4, heads, hd, generator=c.g)
     kv[0], kv[1, :, ::3], kv[2, :, 1::2], kv[3] = math.nan, math.inf, -math.inf, math.nan
     c.set_rows(0, [past + b for b in bad], k=torch.where(torch.isnan(kv), kv, torch.full_like(kv, math.nan)), v=kv)
-    end = c.table.shape[1] * m.PAGE
     behind = [x for x in range(past + n, -(-(past + n) // m.PAGE) * m.PAGE)]
     junk = torch.full((len(behind), heads, hd), math.nan)
     c.set_rows(0, behind, k=junk, v=junk)
     words = m.tree_words(c.g, [n, 9])
     hide = ~sum(1 << b for b in bad)
     words = [w & hide if t < n else w for t, w in enumerate(words)]
-    q = c.randn(c.T, heads * hd)
-    out, lse = torch.empty_like(q), torch.empty(c.T, heads, device=m.DEV)
-    c.ctx.attend(0, c.lens, c.d_past, c.d_table, q, out, visible=m.word_tensor(words), lse=lse)
-    torch.cuda.synchronize()
-    m.check_attention(c, q, 1, out, lse, words)
-    assert torch.isfinite(out).all() or past == 0
+    nq = heads * group
+    q = c.randn(c.T, nq * hd)
+    out, lse = torch.empty_like(q), torch.empty(c.T, nq, device=m.DEV)
+
+    def run(words):
+        c.ctx.attend(0, c.lens, c.d_past, c.d_table, q, out, visible=m.word_tensor(words), lse=lse)
+        torch.cuda.synchronize()
+        m.check_attention(c, q, group, out, lse, words)
+
+    run(words)
+    assert torch.isfinite(out).all()
     # values alone: the keys are fine, tokens 0 .. 4 see the infinite value
     c.set_rows(0, [past + b for b in bad], k=torch.randn(4, heads, hd, generator=c.g))
     words = [w | (1 << 11) if t < 5 else w for t, w in enumerate(words)]
-    c.ctx.attend(0, c.lens, c.d_past, c.d_table, q, out, visible=m.word_tensor(words), lse=lse)
-    m.check_attention(c, q, 1, out, lse, words)
-    o = out[:5].view(5, heads, hd)
-    assert torch.isinf(o[..., ::3]).all() and torch.isfinite(o[..., 1::3]).all()
-    # and a key that is not a number, where it is seen
+    run(words)
+    o = out[:5].view(5, nq, hd)
+    assert torch.isinf(o[..., ::3]).all() and torch.isfinite(o[..., 1::3]).all() and torch.isfinite(out[5:]).all()
+    # tokens 5 and 6 see both infinities (NaN where they meet), token 7 the NaN
+    words = [w | (1 << 11) | (1 << 12) if t in (5, 6) else w | (1 << 29) if t == 7 else w for t, w in enumerate(words)]
+    run(words)
+    assert torch.isnan(out[7]).all() and torch.isnan(out[5].view(nq, hd)[:, 3::6]).all() and torch.isfinite(out[8:]).all()
+    # a key that is not a number, where it is seen
     c.set_rows(0, [past + 12], k=torch.full((1, heads, hd), math.nan))
-    words = [w | (1 << 12) if t == 6 else w for t, w in enumerate(words)]
+    words = [w | (1 << 12) if t == 8 else w for t, w in enumerate(words)]
     c.ctx.attend(0, c.lens, c.d_past, c.d_table, q, out, visible=m.word_tensor(words), lse=lse)
-    assert torch.isnan(out[6]).all() and torch.isnan(lse[6]).all() and torch.isfinite(out[7:]).all() == (past > 0 or bool(torch.isfinite(out[7:]).all()))
+    assert torch.isnan(out[8]).all() and torch.isnan(lse[8]).all() and torch.isfinite(out[9:]).all()
     c.close()
 
 
