@@ -419,8 +419,9 @@ class Context:
     # ---- operators on the paged cache (shapes: T = sum(lens) rows; see include/dinfer.h)
     def _rows(self, name, t, heads):
         """Address and stride of a [T][heads * head_dim] matrix, rows contiguous."""
-        if t.dtype is not self._dtype or t.dim() != 2 or t.shape[1] != heads * self.cfg.head_dim or t.stride(1) != 1:
-            raise ValueError("%s must be a [T][%d] tensor of the context's dtype with contiguous rows" % (name, heads * self.cfg.head_dim))
+        width = heads * self.cfg.head_dim
+        if t.dtype is not self._dtype or t.shape[1:] != (width,) or t.stride(1) != 1:
+            raise ValueError("%s must be a [T][%d] tensor of the context's dtype with contiguous rows" % (name, width))
         return t.data_ptr(), t.stride(0)
 
     def kv_append(self, layer, lens, d_past, d_page_table, d_q, d_k, d_v, d_q_out, q_gain=None, k_gain=None, eps=1e-6,

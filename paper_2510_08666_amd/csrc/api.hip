@@ -215,7 +215,7 @@ Workspace map_workspace(const dinfer_config& c, int max_seqs, int max_tokens) {
   w.conf = cv.take(T * 4);
   w.argmax = cv.take(T * 4);
   w.tok_rot = cv.take(T * 4);                    // rotary positions of a forward over a shortened cache
-  w.attend_part = cv.take(attend_part_bytes(c.head_dim, c.max_pos));
+  w.attend_part = cv.take(attend_part_bytes(c.dtype == DINFER_BF16, c.head_dim, c.max_pos));
   w.score_lse = cv.take(T * c.n_heads * 4);      // normalisers of a scored step's rows
   w.total = cv.at;
   return w;

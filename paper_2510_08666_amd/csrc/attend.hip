@@ -112,10 +112,13 @@ __device__ inline float log_sum(float m, float l) { return l == 0.f ? -INFINITY 
 // the device, so every wave works the plan out for itself, a lane per sequence.  A part has `per` key tiles at most: with few pairs as
 // many as leave about as many parts as workgroups run at a time, counting half a part per pair for the rounding (a few
 // workgroups more than fit run alone behind the others: 16 sequences of 17 to 32 tokens behind 256 to 2048, 608 of them 39.6 us, 496
-// 36.9); with many pairs the compute units' share of all tiles, the longest parts first, so that the short ones fill the gaps; and at least
-// MIN_PART (two per wave).  A pair of up to MIN_CUT tiles is left whole: its waves have most of what they need under way at once, and joining
-// costs more than they take.
-constexpr int ATTEND_MIN_CUT = 24, ATTEND_MIN_PART = 8, ATTEND_WAVES = 4;
+// 36.9); with many pairs the workgroups' share of all tiles, the longest parts first, so that the short ones fill the gaps; and at
+// least min_part (64 drafts behind 4096 keys: 8 tiles 22.9 us, 12 18.7).  A pair of up to min_cut tiles is left whole: its waves
+// have most of what they need under way at once, and joining costs more than they take.
+// In float32 a tile keeps a wave's matrix unit busy for 1.7 us: a pair is cut much earlier (3 sequences behind 64 to 901 keys 20.4 -> 12.3 us).
+template <typename E> constexpr int min_cut() { return sizeof(E) == 2 ? 24 : 8; }
+template <typename E> constexpr int min_part() { return sizeof(E) == 2 ? 12 : 4; }
+constexpr int ATTEND_WAVES = 4;
 struct Plan {
   int seq, base, tiles, groups, parts;      // of this lane's sequence
   uint32_t end, slot_end, cut_end;          // sums, up to this lane's sequence, of workgroups, partial results, pairs that were cut
@@ -123,7 +126,7 @@ struct Plan {
 };
 // Workgroups that run at the same time: two per compute unit, one of those with eight row tiles.
 constexpr int resident(int rows) { return rows > 128 ? 256 : 512; }
-template <int ROWS> __device__ inline Plan make_plan(const AttendArgs& a) {
+template <typename E, int ROWS> __device__ inline Plan make_plan(const AttendArgs& a) {
   constexpr int PARTS = resident(ROWS);
   const int lane = threadIdx.x & 63, s = min(lane, a.tok.span.n_seq - 1);
   const int len = lane == s ? a.tok.span.off[s + 1] - a.tok.span.off[s] : 0;
@@ -136,8 +139,8 @@ template <int ROWS> __device__ inline Plan make_plan(const AttendArgs& a) {
   const uint32_t all_pairs = __builtin_amdgcn_readlane(lane_scan(pairs), WAVE - 1);
   const bool many = all_pairs > PARTS / 2;
   const uint32_t aim = many ? PARTS : PARTS - all_pairs / 2;
-  const int per = max((int)((units + aim - 1) / aim), ATTEND_MIN_PART);
-  p.parts = a.whole || p.tiles <= ATTEND_MIN_CUT ? 1 : (p.tiles + per - 1) / per;
+  const int per = max((int)((units + aim - 1) / aim), min_part<E>());
+  p.parts = a.whole || p.tiles <= min_cut<E>() ? 1 : (p.tiles + per - 1) / per;
   p.seq = lane;
   if (many && a.tok.span.n_seq > 1) {
     // the longest parts first
@@ -242,7 +245,7 @@ __global__ __launch_bounds__(ATTEND_WAVES * WAVE, (attend_waves_per_simd<E, HD>(
   vec* qs = reinterpret_cast<vec*>(smem) + rt * (DSTEPS * NP * WAVE);                            // [RG][k-step][plane][64 lanes]
   int32_t* pt = reinterpret_cast<int32_t*>(smem + RG * DSTEPS * NP * WAVE * 16);                 // page ids of the piece
   float* lds = reinterpret_cast<float*>(smem);      // behind the key tiles: [ATTEND_WAVES][REGS, then m, l][64 lanes]
-  const Plan plan = make_plan<ROWS>(a);
+  const Plan plan = make_plan<E, ROWS>(a);
   const uint32_t wg = near_workgroup();
   if (wg >= plan.total) return;
   const Piece c = piece_at(plan, wg, a.geom.n_heads);
@@ -455,8 +458,9 @@ __global__ __launch_bounds__(ATTEND_WAVES * WAVE, (attend_waves_per_simd<E, HD>(
 // each wave would fetch it for itself, and the compute unit's cache bounds the launch (48 sequences of 31 to 64 tokens with four
 // query heads per cache head behind 1000 to 8000: 467 us).  A wave keeps its queries and output in registers, nothing is folded.
 // Bound by the read of K and V, so a workgroup takes up to 256 rows (four waves and 128 rows, two workgroups per compute unit: 300 to
-// 370 us, 1.35 GB fetched).  Of the two waves of a SIMD one has priority, so that it works on its softmax while the other
-// multiplies; in step they would do both one after the other.
+// 370 us, 1.35 GB fetched; eight waves 263).  What a turn takes now, 2.4 us, is none of its bounds alone (counters: matrix units busy
+// 31 % of the time, LDS 22 %): waves wait for each other.  Without effect: two turns of loads under way, priorities or half a
+// turn's distance between the waves of a SIMD, output products between the second tile's exponentials, deeper rings.
 template <int HD> constexpr size_t attend_rows_lds() { return (size_t)2 * 4 * (HD / ET<bf16_t>::KS) * WAVE * 16 + ATTN_MAX_PAGES * 4; }
 template <int HD, int WAVES>
 __global__ __launch_bounds__(WAVES * WAVE, 2) void attend_rows_kernel(AttendArgs a, const int32_t* __restrict__ live) {
@@ -473,7 +477,7 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void attend_rows_kernel(AttendArgs
   auto kv = reinterpret_cast<vec(*)[4][WF][WAVE]>(smem);      // [buffer][K of tile 0, K of tile 1, V of 0, V of 1][fragment][lane]
   int32_t* pt = reinterpret_cast<int32_t*>(smem + (size_t)2 * 4 * WF * WAVE * 16);
   __shared__ int32_t odd_turn[2];      // of a buffer: some value of a new token is no finite number
-  const Plan plan = make_plan<ROWS>(a);
+  const Plan plan = make_plan<E, ROWS>(a);
   const uint32_t wg = near_workgroup();
   if (wg >= plan.total) return;
   const Piece c = piece_at(plan, wg, a.geom.n_heads);
@@ -619,7 +623,6 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void attend_rows_kernel(AttendArgs
   };
   // The turns in front of the tail, and the one before it, whose neighbour has to be masked on its way to LDS.
   const int full = (min(c.base, last_key + 1) - kt0 * TILE) / (2 * TILE);
-  if (SHARE == 2 && wave < 4) __builtin_amdgcn_s_setprio(1);
   fetch(0);
   put(0, std::true_type{});
   fetch(1);
@@ -733,8 +736,8 @@ template <typename E, int HD, int NP, int RG, bool PV> constexpr size_t attend_l
   const size_t walk = (size_t)RG * (HD / ET<E>::KS) * NP * WAVE * 16 + ATTN_MAX_PAGES * 4;
   return fold > walk ? fold : walk;
 }
-size_t attend_part_bytes(int head_dim, int max_pos) {
-  if (max_pos <= ATTEND_MIN_CUT * TILE) return 0;      // nothing is cut
+size_t attend_part_bytes(bool bf16, int head_dim, int max_pos) {
+  if (max_pos <= (bf16 ? min_cut<bf16_t>() : min_cut<float>()) * TILE) return 0;      // nothing is cut
   const size_t rows = (size_t)2 * resident(8 * TILE) * 8 * TILE, few = (size_t)2 * resident(4 * TILE) * 4 * TILE;
   return (rows > few ? rows : few) * (head_dim + 2) * 4 + sizeof(CutList);
 }
@@ -743,11 +746,11 @@ size_t attend_part_bytes(int head_dim, int max_pos) {
 struct AttendGrid {
   unsigned wgs, cut;
 };
-template <int ROWS> static AttendGrid attend_grid(AttendArgs& a) {
+template <typename E, int ROWS> static AttendGrid attend_grid(AttendArgs& a) {
   int64_t pairs = 0;
   for (int s = 0; s < a.tok.span.n_seq; ++s) pairs += ((int64_t)(a.tok.span.off[s + 1] - a.tok.span.off[s]) * a.group + ROWS - 1) / ROWS;
   pairs *= a.geom.n_heads;
-  a.whole = single_slice() || a.tok.limit <= ATTEND_MIN_CUT * TILE;
+  a.whole = single_slice() || a.tok.limit <= min_cut<E>() * TILE;
   const int64_t wgs = a.whole ? pairs : pairs + resident(ROWS);
   return AttendGrid{(unsigned)((wgs + 31) / 32 * 32), a.whole ? 0u : (unsigned)(pairs < resident(ROWS) ? pairs : resident(ROWS))};
 }
@@ -755,12 +758,12 @@ template <typename E, int HD, int ROWS, bool PV> static void launch_merge(const 
   if (cut > 0) attend_merge_kernel<E, HD, ROWS, PV><<<cut * (ROWS / (merge_rows<HD, PV>() * (ROWS > 64 ? 4 : 1))), MERGE_THREADS, 0, st>>>(a, live_word());
 }
 template <typename E, int HD, int NP, int RG, bool PV> static void launch_attend_t(AttendArgs a, hipStream_t st) {
-  const AttendGrid g = attend_grid<RG * TILE>(a);
+  const AttendGrid g = attend_grid<E, RG * TILE>(a);
   attend_kernel<E, HD, NP, RG, PV><<<g.wgs, ATTEND_WAVES * WAVE, attend_lds<E, HD, NP, RG, PV>(), st>>>(a, live_word());
   launch_merge<E, HD, RG * TILE, PV>(a, g.cut, st);
 }
 template <int HD, int WAVES> static void launch_attend_rows(AttendArgs a, hipStream_t st) {
-  const AttendGrid g = attend_grid<WAVES * TILE>(a);
+  const AttendGrid g = attend_grid<bf16_t, WAVES * TILE>(a);
   attend_rows_kernel<HD, WAVES><<<g.wgs, WAVES * WAVE, attend_rows_lds<HD>(), st>>>(a, live_word());
   launch_merge<bf16_t, HD, WAVES * TILE, true>(a, g.cut, st);
 }
@@ -769,7 +772,9 @@ template <typename E, int HD, int RG> static void launch_attend_rg(int planes, c
   else if (planes == 1) launch_attend_t<E, HD, 1, RG, false>(a, st);
   else if constexpr (sizeof(E) == 2) launch_attend_t<E, HD, 2, RG, false>(a, st);
 }
-// Two row tiles per workgroup where a sequence has more than one; more than two: the form whose tiles go through LDS (bfloat16).
+// Two row tiles per workgroup where a sequence has more than one; more than two: the form whose tiles go through LDS.  In float32 the
+// matrix instructions are the bound (a sixteenth of the rate), not the reads that row tiles could share: one tile per workgroup (3
+// sequences of 5 to 33 tokens 28.9 -> 20.4 us).
 template <int HD> static void launch_attend_hd(bool bf16, int planes, const AttendArgs& a, hipStream_t st) {
   const int most = most_rows(a.tok.span, a.group);
   if (bf16) {
@@ -777,10 +782,7 @@ template <int HD> static void launch_attend_hd(bool bf16, int planes, const Atte
     else if (most > 2 * TILE && a.out) launch_attend_rows<HD, 4>(a, st);
     else if (most <= TILE) launch_attend_rg<bf16_t, HD, 1>(planes, a, st);
     else launch_attend_rg<bf16_t, HD, 2>(planes, a, st);
-  } else {
-    if (most <= TILE) launch_attend_rg<float, HD, 1>(planes, a, st);
-    else launch_attend_rg<float, HD, 2>(planes, a, st);
-  }
+  } else launch_attend_rg<float, HD, 1>(planes, a, st);
 }
 void launch_attend(bool bf16, int planes, const AttendArgs& a, hipStream_t st) {
   if (a.geom.head_dim == 128) launch_attend_hd<128>(bf16, planes, a, st);
@@ -796,8 +798,8 @@ template <int HD, int WAVES> static bool configure_rows() {
 }
 bool configure_attend() {
   const bool ok = configure_attend_t<bf16_t, 128, 1>() && configure_attend_t<bf16_t, 128, 2>() && configure_attend_t<bf16_t, 64, 1>() &&
-                  configure_attend_t<bf16_t, 64, 2>() && configure_attend_t<float, 128, 1>() && configure_attend_t<float, 128, 2>() &&
-                  configure_attend_t<float, 64, 1>() && configure_attend_t<float, 64, 2>() && configure_rows<128, 4>() &&
+                  configure_attend_t<bf16_t, 64, 2>() && configure_attend_t<float, 128, 1>() && configure_attend_t<float, 64, 1>() &&
+                  configure_rows<128, 4>() &&
                   configure_rows<128, 8>() && configure_rows<64, 4>() && configure_rows<64, 8>();
   (void)hipGetLastError();
   return ok;

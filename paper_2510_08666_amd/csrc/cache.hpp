@@ -87,7 +87,7 @@ struct AttendArgs {
   float* part;                // attend_part_bytes
   bool whole;                 // set by the launch: no pair's keys are cut
 };
-size_t attend_part_bytes(int head_dim, int max_pos);
+size_t attend_part_bytes(bool bf16, int head_dim, int max_pos);
 // planes: of the queries (two: the forward's own bfloat16 queries, normalisers only).
 void launch_attend(bool bf16, int planes, const AttendArgs& a, hipStream_t st);
 
