@@ -227,7 +227,8 @@ def make_config(cfg, max_pos):
 
 
 def _stream():
-    return torch.cuda.current_stream().cuda_stream
+    """Handle of the current stream (without the Stream object around it, which takes longer than a small kernel)."""
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _ptr(t):

@@ -296,13 +296,11 @@ void score_layer(dinfer_ctx* c, const SeqSpan& span, const int32_t* d_base, int 
   const CacheTokens tok{span, d_base, limit, d_page_table, pt_stride};
   const float scale = 1.f / sqrtf((float)f.head_dim);
   float* lse = at<float>(c->ws, c->wsm.score_lse);
-  AttendArgs aa{tok, kv_layer, c->geom, c->ws + c->wsm.q, D, q_plane, 1, nullptr, scale, nullptr, 0, lse,
-                at<float>(c->ws, c->wsm.attend_part), false};
-  launch_attend(c->bf16, planes, aa, st);
   const int64_t layer_scores = (int64_t)span.n_seq * f.n_heads * use.score_stride * l;
-  launch_score(c->bf16, planes,
-               ScoreArgs{tok, kv_layer, c->geom, c->ws + c->wsm.q, D, q_plane, 1, nullptr, scale, lse, use.decay,
-                         use.d_score_in ? use.d_score_in + layer_scores : nullptr, use.d_score_out + layer_scores, use.score_stride}, st);
+  launch_normalised_score(c->bf16, planes,
+                          ScoreArgs{tok, kv_layer, c->geom, c->ws + c->wsm.q, D, q_plane, 1, nullptr, scale, lse, use.decay,
+                                    use.d_score_in ? use.d_score_in + layer_scores : nullptr, use.d_score_out + layer_scores, use.score_stride},
+                          lse, at<float>(c->ws, c->wsm.attend_part), st);
 }
 
 // One forward over the packed tokens of `span`.  with_head: an LM head follows (LmArgs::xn_hi is wanted).
@@ -1207,12 +1205,8 @@ int dinfer_kv_score(dinfer_ctx* c, int32_t layer, int32_t n_seq, const int32_t* 
   a.decay = decay;
   a.score_in = d_score_in, a.score_out = d_score_out, a.score_stride = score_stride;
   if (a.tok.span.off[n_seq] == 0) return DINFER_OK;
-  if (!lse_given) {
-    AttendArgs n{a.tok, a.kv_layer, a.geom, d_q, q_stride, 0, a.group, d_visible, a.scale, nullptr, 0, d_lse,
-                 at<float>(c->ws, c->wsm.attend_part), false};
-    launch_attend(c->bf16, 1, n, (hipStream_t)stream);
-  }
-  launch_score(c->bf16, 1, a, (hipStream_t)stream);
+  if (lse_given) launch_score(c->bf16, 1, a, (hipStream_t)stream);
+  else launch_normalised_score(c->bf16, 1, a, d_lse, at<float>(c->ws, c->wsm.attend_part), (hipStream_t)stream);
   HIP_TRY(hipGetLastError());
   return DINFER_OK;
 }

@@ -107,6 +107,8 @@ struct ScoreArgs {
   int32_t score_stride;
 };
 void launch_score(bool bf16, int planes, const ScoreArgs& a, hipStream_t st);
+// The same with normalisers that are worked out on the way and left in lse (= a.lse); part as in AttendArgs.
+void launch_normalised_score(bool bf16, int planes, const ScoreArgs& a, float* lse, float* part, hipStream_t st);
 
 struct EvictArgs {
   void* kv;                   // of the first layer
