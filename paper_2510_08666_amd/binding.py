@@ -269,6 +269,7 @@ class Context:
             raise DinferError(-1, last_error())
         self.n_pages, self.max_seqs, self.max_tokens = n_pages, max_seqs, max_tokens
         self._dtype = torch.bfloat16 if self.ccfg.dtype == BF16 else torch.float32
+        self._index = self.device.index if self.device.index is not None else torch.cuda.current_device()
         if weights_buffer is not None:
             if weights_buffer.numel() < wb or weights_buffer.device != self.device:
                 raise ValueError("weights_buffer does not fit this configuration")
@@ -418,62 +419,99 @@ class Context:
         return run.value
 
     # ---- operators on the paged cache (shapes: T = sum(lens) rows; see include/dinfer.h)
-    def _rows(self, name, t, heads):
-        """Address and stride of a [T][heads * head_dim] matrix, rows contiguous."""
+    def _raw_stream(self):
+        return torch._C._cuda_getCurrentRawStream(self._index)
+
+    def _rows(self, name, t, rows, heads):
+        """Address and stride of a matrix of at least `rows` rows of heads * head_dim contiguous elements."""
         width = heads * self.cfg.head_dim
-        if t.dtype is not self._dtype or t.shape[1:] != (width,) or t.stride(1) != 1:
-            raise ValueError("%s must be a [T][%d] tensor of the context's dtype with contiguous rows" % (name, width))
-        return t.data_ptr(), t.stride(0)
+        if t.dtype is self._dtype and t.dim() == 2 and t.get_device() == self._index:
+            (n, m), (stride, one) = t.shape, t.stride()
+            if n >= rows and m == width and one == 1:
+                return t.data_ptr(), stride
+        raise ValueError("%s must be a [%d][%d] tensor of the context's dtype and device, rows contiguous" % (name, rows, width))
+
+    def _flat(self, name, t, dtype, *shape):
+        """Address of a contiguous tensor of that type and these sizes (the first may be larger); None passes."""
+        if t is None:
+            return None
+        if t.dtype is dtype and t.get_device() == self._index and t.is_contiguous():
+            n = t.shape
+            if n == shape or (len(n) == len(shape) and n[0] >= shape[0] and n[1:] == shape[1:]):
+                return t.data_ptr()
+        raise ValueError("%s must be a contiguous %s tensor %s on the context's device" % (name, dtype, list(shape)))
+
+    def _tokens(self, lens, d_past, d_page_table):
+        """The arguments that say which tokens join which sequences, and how many there are."""
+        n = len(lens)
+        return ((n, (c_i32 * n)(*lens), self._flat("d_past", d_past, torch.int32, n),
+                 self._flat("d_page_table", d_page_table, torch.int32, n, d_page_table.shape[1]), d_page_table.shape[1]), sum(lens))
+
+    def _words(self, visible, T):
+        if visible is not None and visible.dtype is torch.uint64:
+            visible = visible.view(torch.int64)
+        return self._flat("visible", visible, torch.int64, T)
 
     def kv_append(self, layer, lens, d_past, d_page_table, d_q, d_k, d_v, d_q_out, q_gain=None, k_gain=None, eps=1e-6,
                   rotary=None, rotary_table=None, positions=None):
         """Norms, rotates and stores a layer's new tokens; d_q_out receives the queries (d_q and d_q_out None: keys and values only)."""
-        n, nh = len(lens), self.cfg.n_heads
-        k, v = self._rows("d_k", d_k, nh), self._rows("d_v", d_v, nh)
-        nq = nh if d_q is None else d_q.shape[1] // self.cfg.head_dim
-        q, out = ((None, 0), (None, 0)) if d_q is None else (self._rows("d_q", d_q, nq), self._rows("d_q_out", d_q_out, nq))
-        _check(lib.dinfer_kv_append(self.h, layer, n, (c_i32 * n)(*lens), _ptr(d_past), _ptr(d_page_table), d_page_table.shape[1],
-                                    q[0], q[1], k[0], k[1], v[0], v[1], nq, _ptr(q_gain), _ptr(k_gain), eps, rotary,
-                                    _ptr(rotary_table), 0 if rotary_table is None else rotary_table.shape[1], _ptr(positions),
-                                    out[0], out[1], _stream()))
+        tok, T = self._tokens(lens, d_past, d_page_table)
+        nh, hd = self.cfg.n_heads, self.cfg.head_dim
+        nq = nh if d_q is None else d_q.shape[1] // hd
+        q, out = ((None, 0), (None, 0)) if d_q is None else (self._rows("d_q", d_q, T, nq), self._rows("d_q_out", d_q_out, T, nq))
+        table_positions = 0
+        if rotary is not None and rotary_table is not None:
+            table_positions = rotary_table.shape[1]
+            self._flat("rotary_table", rotary_table, torch.float32, 2, table_positions, rotary.rotary_dim // 2)
+        _check(lib.dinfer_kv_append(self.h, layer, *tok, *q, *self._rows("d_k", d_k, T, nh), *self._rows("d_v", d_v, T, nh), nq,
+                                    self._flat("q_gain", q_gain, torch.float32, hd), self._flat("k_gain", k_gain, torch.float32, hd), eps,
+                                    rotary, _ptr(rotary_table), table_positions, self._flat("positions", positions, torch.int32, T),
+                                    *out, self._raw_stream()))
 
     def attend(self, layer, lens, d_past, d_page_table, d_q, d_out, visible=None, scale=0.0, lse=None):
         """Attention of the new tokens over the cache, their own keys as far as the words of `visible` [T] allow."""
-        n, nq = len(lens), d_q.shape[1] // self.cfg.head_dim
-        q, out = self._rows("d_q", d_q, nq), self._rows("d_out", d_out, nq)
-        _check(lib.dinfer_attend(self.h, layer, n, (c_i32 * n)(*lens), _ptr(d_past), _ptr(d_page_table), d_page_table.shape[1],
-                                 q[0], q[1], nq, _ptr(visible), scale, out[0], out[1], _ptr(lse), _stream()))
+        tok, T = self._tokens(lens, d_past, d_page_table)
+        nq = d_q.shape[1] // self.cfg.head_dim
+        _check(lib.dinfer_attend(self.h, layer, *tok, *self._rows("d_q", d_q, T, nq), nq, self._words(visible, T), scale,
+                                 *self._rows("d_out", d_out, T, nq), self._flat("lse", lse, torch.float32, T, nq), self._raw_stream()))
 
     def kv_score(self, layer, lens, d_past, d_page_table, d_q, d_score_out, score_in=None, decay=1.0, visible=None, scale=0.0,
                  lse=None):
         """Adds the attention weight of the new tokens to d_score_out [n_seq][n_heads][stride]; lse: what `attend` left for
         the same queries (None: worked out here)."""
-        n, nq = len(lens), d_q.shape[1] // self.cfg.head_dim
-        q = self._rows("d_q", d_q, nq)
+        tok, T = self._tokens(lens, d_past, d_page_table)
+        nq, shape = d_q.shape[1] // self.cfg.head_dim, (len(lens), self.cfg.n_heads, d_score_out.shape[2])
+        q = self._rows("d_q", d_q, T, nq)
         given = lse is not None
         if not given:
-            lse = torch.empty((d_q.shape[0], nq), dtype=torch.float32, device=d_q.device)
-        _check(lib.dinfer_kv_score(self.h, layer, n, (c_i32 * n)(*lens), _ptr(d_past), _ptr(d_page_table), d_page_table.shape[1],
-                                   q[0], q[1], nq, _ptr(visible), scale, _ptr(lse), given, decay, _ptr(score_in),
-                                   _ptr(d_score_out), d_score_out.shape[2], _stream()))
+            lse = torch.empty((max(T, 1), nq), dtype=torch.float32, device=d_q.device)
+        _check(lib.dinfer_kv_score(self.h, layer, *tok, *q, nq, self._words(visible, T), scale, self._flat("lse", lse, torch.float32, T, nq),
+                                   given, decay, self._flat("score_in", score_in, torch.float32, *shape),
+                                   self._flat("d_score_out", d_score_out, torch.float32, *shape), shape[2], self._raw_stream()))
 
     def kv_evict(self, first_layer, n_layers, keep, n_sink, n_recent, d_score, d_len, d_page_table, d_new_page_table, d_kept,
                  d_new_len, score_out=None):
         """Keeps `keep` positions per (layer, sequence, head) of d_score [n_layers][n_seq][n_heads][stride] in new pages."""
-        _check(lib.dinfer_kv_evict(self.h, first_layer, n_layers, d_page_table.shape[0], keep, n_sink, n_recent, _ptr(d_score),
-                                   d_score.shape[3], _ptr(d_len), _ptr(d_page_table), d_page_table.shape[1],
-                                   _ptr(d_new_page_table), d_new_page_table.shape[1], _ptr(d_kept), _ptr(score_out),
-                                   _ptr(d_new_len), _stream()))
+        ns, nh, width = d_page_table.shape[0], self.cfg.n_heads, d_score.shape[3]
+        i32 = torch.int32
+        _check(lib.dinfer_kv_evict(self.h, first_layer, n_layers, ns, keep, n_sink, n_recent,
+                                   self._flat("d_score", d_score, torch.float32, n_layers, ns, nh, width), width,
+                                   self._flat("d_len", d_len, i32, ns), self._flat("d_page_table", d_page_table, i32, *d_page_table.shape),
+                                   d_page_table.shape[1], self._flat("d_new_page_table", d_new_page_table, i32, ns, d_new_page_table.shape[1]),
+                                   d_new_page_table.shape[1], self._flat("d_kept", d_kept, i32, n_layers, ns, nh, keep),
+                                   self._flat("score_out", score_out, torch.float32, n_layers, ns, nh, width),
+                                   self._flat("d_new_len", d_new_len, i32, ns), self._raw_stream()))
 
-    @staticmethod
-    def _cache_use(position, score_in, score_out, decay):
-        return CacheUse(_ptr(position), _ptr(score_in), _ptr(score_out), 0 if score_out is None else score_out.shape[3], decay)
+    def _cache_use(self, n_seq, position, score_in, score_out, decay):
+        shape = (self.cfg.n_layers, n_seq, self.cfg.n_heads, 0 if score_out is None else score_out.shape[3])
+        return CacheUse(self._flat("position", position, torch.int32, n_seq), self._flat("score_in", score_in, torch.float32, *shape),
+                        self._flat("score_out", score_out, torch.float32, *shape), shape[3], decay)
 
     def step_scored(self, d_block_tokens, d_mask, d_prefix_len, d_page_table, threshold, fixed_k, d_conf, d_argmax,
                     d_n_committed, position=None, score_in=None, score_out=None, decay=1.0):
         """step over a cache that may have been shortened; score_out [n_layers][n_seq][n_heads][stride] receives its scores."""
         n_seq, block_len = d_block_tokens.shape
-        dec, use = _decode(threshold, fixed_k), self._cache_use(position, score_in, score_out, decay)
+        dec, use = _decode(threshold, fixed_k), self._cache_use(n_seq, position, score_in, score_out, decay)
         _check(lib.dinfer_step_scored(self.h, n_seq, block_len, _ptr(d_block_tokens), _ptr(d_mask), _ptr(d_prefix_len),
                                       _ptr(d_page_table), d_page_table.shape[1], ctypes.byref(dec), ctypes.byref(use),
                                       _ptr(d_conf), _ptr(d_argmax), _ptr(d_n_committed), _stream()))
@@ -481,7 +519,7 @@ class Context:
     def refresh_block_scored(self, d_block_tokens, d_prefix_len, d_page_table, position=None, score_in=None, score_out=None,
                              decay=1.0):
         n_seq, block_len = d_block_tokens.shape
-        use = self._cache_use(position, score_in, score_out, decay)
+        use = self._cache_use(n_seq, position, score_in, score_out, decay)
         _check(lib.dinfer_refresh_block_scored(self.h, n_seq, block_len, _ptr(d_block_tokens), _ptr(d_prefix_len),
                                                _ptr(d_page_table), d_page_table.shape[1], ctypes.byref(use), _stream()))
 

@@ -264,13 +264,25 @@ def test_refusals(m):
         refused(fn, base, -1, layer=1)
         refused(fn, base, -1, layer=-1)
         refused(fn, base, -1, lens=[9, -1, 32])
-        refused(fn, base, -1, lens=[9, 0, 32, 0])
-        refused(fn, base, -3, lens=[9, 0, 5000])
+        four = dict(d_past=torch.zeros(4, dtype=torch.int32, device=m.DEV), d_page_table=c.d_table[[0, 1, 2, 0]].contiguous())
+        if fn == ctx.kv_score:
+            four["d_score_out"] = torch.zeros(4, 4, 1200, device=m.DEV)
+        refused(fn, base, -1, lens=[9, 0, 32, 0], **four)                                      # more sequences than the context takes
+        long = torch.zeros(1200, 512, device=m.DEV)
+        refused(fn, base, -3, lens=[9, 0, 1137], d_q=long, **({"d_q_out": long, "d_k": long[:, :256], "d_v": long[:, :256]} if fn == ctx.kv_append else
+                                                             {"d_out": long} if fn == ctx.attend else {}))
+        with pytest.raises(ValueError):
+            fn(**{**base, "lens": [9, 0, 32, 0]})
         refused(fn, base, -1, d_q=torch.zeros(c.T, 6 * 64, device=m.DEV)[:, :5 * 64], **({"d_q_out": b["q"][:, :320]} if fn == ctx.kv_append else
                                                                                  {"d_out": b["q"][:, :320]} if fn == ctx.attend else {}))
         refused(fn, base, -1, d_q=torch.zeros(c.T * 512 + 1, device=m.DEV)[1:].view(c.T, 512))            # not 16-byte aligned
+        for bad in (b["q"].half(), b["q"].cpu(), b["q"][:-1], b["q"].t(), b["q"][:, ::2]):           # type, device, rows, layout
+            with pytest.raises(ValueError):
+                fn(**{**base, "d_q": bad})
         with pytest.raises(ValueError):
-            fn(**{**base, "d_q": b["q"].half()})
+            fn(**{**base, "d_past": c.d_past.long()})
+        with pytest.raises(ValueError):
+            fn(**{**base, "d_page_table": c.d_table.t()})
     many = torch.zeros(65, 512, device=m.DEV)
     refused(ctx.attend, attend, -1, lens=[65, 0, 0], d_q=many, d_out=many, visible=torch.zeros(65, dtype=torch.int64, device=m.DEV))
     for bad in (-1.0, float("nan"), float("inf")):
@@ -279,12 +291,23 @@ def test_refusals(m):
         refused(ctx.kv_score, score, -1, decay=bad)
         refused(ctx.kv_append, append, -1, eps=bad, q_gain=b["gain"])
     refused(ctx.kv_append, append, -1, rotary=rot(48, False))                                              # no table
-    refused(ctx.kv_append, append, -1, rotary=rot(66, False), rotary_table=b["tab"])
-    refused(ctx.kv_append, append, -1, rotary=rot(47, False), rotary_table=b["tab"])
+    for dim in (66, 47):                                                                                   # more than a head, odd
+        refused(ctx.kv_append, append, -1, rotary=rot(dim, False), rotary_table=torch.zeros(2, 1200, dim // 2, device=m.DEV))
     for kw in (dict(keep=0), dict(n_sink=-1), dict(n_sink=60, n_recent=50), dict(n_layers=2), dict(first_layer=1), dict(d_new_page_table=c.d_table),
                dict(score_out=b["score"][None]), dict(d_new_len=b["len"]), dict(keep=100000)):
+        layers, keep = kw.get("n_layers", 1), kw.get("keep", 100)
+        if layers > 1 or keep != 100:                      # tensors that fit the refused number
+            kw = dict(kw, d_score=b["score"][None].expand(layers, -1, -1, -1).contiguous(), d_kept=torch.zeros(layers, 3, 4, keep, dtype=torch.int32, device=m.DEV))
         refused(ctx.kv_evict, evict, -1, **kw)
     refused(ctx.kv_evict, evict, -3, keep=113, d_kept=torch.zeros(1, 3, 4, 113, dtype=torch.int32, device=m.DEV))      # seven new pages hold 112
+    for fn, base, kw in ((ctx.kv_append, append, dict(q_gain=b["gain"].double())), (ctx.kv_append, append, dict(k_gain=b["gain"][:60])),
+                         (ctx.kv_append, append, dict(positions=b["len"])), (ctx.kv_append, append, dict(rotary=rot(64), rotary_table=b["tab"])),
+                         (ctx.attend, attend, dict(visible=words[:-1])), (ctx.attend, attend, dict(lse=b["lse"][:-1])),
+                         (ctx.kv_score, score, dict(lse=b["lse"][:, :4])), (ctx.kv_score, score, dict(score_in=b["score"][:, :, :100])),
+                         (ctx.kv_evict, evict, dict(d_kept=b["kept"][..., :99])), (ctx.kv_evict, evict, dict(d_len=b["len"][:2])),
+                         (ctx.kv_evict, evict, dict(d_score=b["score"][None, :2]))):
+        with pytest.raises(ValueError):
+            fn(**{**base, **kw})
     torch.cuda.synchronize()
     assert torch.equal(c.pool, pool0) and all((b[n] == 0).all() for n in ("lse", "score", "score_out", "kept", "new_len"))
     # nothing to do is no error
