@@ -4,8 +4,9 @@
 // The queries of all query heads that share a cache head are rows of the same contraction (row = token * group + member), so
 // that a tile of 32 rows reads its head's keys once.  MFMA mapping as in attention.hip: S^T[key][row] = K . Q^T, a lane owns
 // one row, O^T[d][row] += V^T . P^T from the score registers.  Queries enter as they are (bfloat16 queries are exact), and
-// probabilities as one bfloat16 plane: their rounding (2^-9 each, independent, weighted by the probabilities themselves) stays below the
-// half step of the bfloat16 output.  Sums of probabilities are those of the unrounded ones.
+// probabilities as one bfloat16 plane: a rounding is off by at most 2^-8 of a probability, they fall either way, and an output is their
+// mean over the keys (error against 64 bits 0.0022 of the outputs, 0.0017 with 32-bit probabilities and the same rounded outputs).  Sums
+// of probabilities are those of the unrounded ones.
 #include <type_traits>
 
 #include "attn_tiles.hpp"
@@ -772,14 +773,25 @@ template <typename E, int HD, int RG> static void launch_attend_rg(int planes, c
   else if (planes == 1) launch_attend_t<E, HD, 1, RG, false>(a, st);
   else if constexpr (sizeof(E) == 2) launch_attend_t<E, HD, 2, RG, false>(a, st);
 }
-// Two row tiles per workgroup where a sequence has more than one; more than two: the form whose tiles go through LDS.  In float32 the
-// matrix instructions are the bound (a sixteenth of the rate), not the reads that row tiles could share: one tile per workgroup (3
-// sequences of 5 to 33 tokens 28.9 -> 20.4 us).
+// Meetings of a row tile with a key tile in a call, at most (the lengths are on the device: as if all caches were full).
+static int64_t most_meetings(const AttendArgs& a) {
+  int64_t row_tiles = 0;
+  for (int s = 0; s < a.tok.span.n_seq; ++s) row_tiles += ((int64_t)(a.tok.span.off[s + 1] - a.tok.span.off[s]) * a.group + TILE - 1) / TILE;
+  return row_tiles * a.geom.n_heads * ((a.tok.limit + TILE - 1) / TILE);
+}
+// Two row tiles per workgroup where a sequence has more than one; more than two: the form whose tiles go through LDS, where there is
+// work enough for it.  Its workgroups are few and take 2.4 us a turn, however little there is: of 8 cache heads of 4 queries each, 60
+// tokens behind 3000 positions take 37.0 us in it and 19.0 in two row tiles, four sequences of them (24 thousand meetings) 45.0
+// and 34.6, eight (49 thousand) 58.8 and 62.0, sixteen 87 and 101; 20, 24 and 16 tokens, 16 and 4 heads and 8 queries per head cross over
+// between 40 and 70 thousand as well.  In float32 the matrix instructions are the bound (a sixteenth of the rate), not the reads that row
+// tiles could share: one tile per workgroup (3 sequences of 5 to 33 tokens 28.9 -> 20.4 us).
+constexpr int64_t ROWS_FORM_MEETINGS = 1 << 16;
 template <int HD> static void launch_attend_hd(bool bf16, int planes, const AttendArgs& a, hipStream_t st) {
   const int most = most_rows(a.tok.span, a.group);
   if (bf16) {
-    if (most > 4 * TILE && a.out) launch_attend_rows<HD, 8>(a, st);
-    else if (most > 2 * TILE && a.out) launch_attend_rows<HD, 4>(a, st);
+    const bool rows_form = most > 2 * TILE && a.out && most_meetings(a) >= ROWS_FORM_MEETINGS;
+    if (rows_form && most > 4 * TILE) launch_attend_rows<HD, 8>(a, st);
+    else if (rows_form) launch_attend_rows<HD, 4>(a, st);
     else if (most <= TILE) launch_attend_rg<bf16_t, HD, 1>(planes, a, st);
     else launch_attend_rg<bf16_t, HD, 2>(planes, a, st);
   } else launch_attend_rg<float, HD, 1>(planes, a, st);
@@ -811,7 +823,8 @@ bool configure_attend() {
 // key's sum over 32 rows is an addition of 16 registers and one exchange between the half-waves, and every score has one writer:
 // no atomics, the same bits every time.  A wave holds KT key tiles in registers, all their loads under way at once, and meets them with
 // one row tile after the other.  Bound by the read of K; with many rows by the matrix instructions and the queries' second
-// reads, which KT tiles share (16 KB of keys per wave: what fits the registers beside the queries).
+// reads, which KT tiles share (16 KB of keys per wave: what fits the registers beside the queries).  16 sequences of 17 to 32 tokens
+// behind 256 to 4096 positions, 150 MB: 34.4 us, 4.3 TB/s with the start of every workgroup (lengths, pages, keys: three dependent loads).
 // ------------------------------------------------------------------------------------------------
 constexpr int SCORE_WAVES = 4;
 // A key's weight over the 16 rows in a lane's registers.  lse: of the tile's rows, times log2(e), infinity for those that weigh nothing;

@@ -14,7 +14,7 @@ TYPE = {"f32": torch.float32, "bf16": torch.bfloat16}
 
 
 class Cache:
-    def __init__(self, dtype, heads, head_dim, lens, past, layers=1, seed=0, spare=2, max_pos=None, room=0):
+    def __init__(self, dtype, heads, head_dim, lens, past, layers=1, seed=0, spare=2, max_pos=None, room=0, columns=0):
         self.dtype, self.nh, self.hd, self.L = dtype, heads, head_dim, layers
         self.lens, self.past, self.ns, self.T = list(lens), list(past), len(lens), sum(lens)
         g = torch.Generator().manual_seed(seed)
@@ -22,7 +22,7 @@ class Cache:
         need = [-(-(l + p + room) // PAGE) + 1 for l, p in zip(lens, past)]
         self.n_pages = sum(need) + spare
         order = torch.randperm(self.n_pages, generator=g).to(torch.int32)
-        self.table = torch.full((self.ns, max(need)), -1, dtype=torch.int32)      # entries that no call may follow
+        self.table = torch.full((self.ns, max(need + [columns])), -1, dtype=torch.int32)      # entries that no call may follow
         at = 0
         for s, n in enumerate(need):
             self.table[s, :n] = order[at:at + n]
@@ -30,7 +30,7 @@ class Cache:
         self.free = order[at:]
         cfg = di.configs.scaled(di.model_preset("tiny"), n_layers=layers, hidden=64, n_heads=heads, head_dim=head_dim, n_experts=1, top_k=1,
                                 moe_inter=64, vocab=64, dtype=dtype)
-        self.ctx = binding.Context(cfg, self.n_pages, self.ns, 64, max_pos or max(need) * PAGE)
+        self.ctx = binding.Context(cfg, self.n_pages, self.ns, 64, max_pos or max(need + [columns]) * PAGE)
         self.pool = self.ctx.kv.view(TYPE[dtype]).view(layers, self.n_pages, 2, -1)
         self.pool.copy_(torch.randn(self.pool.shape, generator=g).to(TYPE[dtype]))
         self.d_table, self.d_past = self.table.to(DEV), torch.tensor(past, dtype=torch.int32, device=DEV)

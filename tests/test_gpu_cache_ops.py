@@ -148,13 +148,10 @@ LENS = [([1, 0, 33, 64, 7], [0, 5, 16, 500, 31]), ([1], [0]), ([1], [2000]), ([6
         ([20, 32, 1, 3, 64, 40], [800, 31, 1600, 0, 4001, 768]), ([3, 0, 7, 64] * 12, [40 * i for i in range(48)])]
 
 
-@pytest.mark.parametrize("dtype,heads,hd", SHAPES)
-@pytest.mark.parametrize("i", range(len(LENS)))
-@pytest.mark.parametrize("kind,group", [("none", 1), ("tree", 1), ("tree", 3), ("causal", 8), ("empty", 2)])
-def test_attend(m, dtype, heads, hd, i, kind, group):
+def attend_case(m, dtype, heads, hd, i, kind, group, columns=0):
     torch = m.torch
     lens, past = LENS[i]
-    c = m.Cache(dtype, heads, hd, lens, past, seed=10 + i)
+    c = m.Cache(dtype, heads, hd, lens, past, seed=10 + i, columns=columns)
     q = c.randn(c.T, heads * group * hd + 16, scale=1.5)[:, :heads * group * hd]
     words = None
     if kind == "tree":
@@ -180,25 +177,36 @@ def test_attend(m, dtype, heads, hd, i, kind, group):
     c.close()
 
 
-def test_attend_long_runs_without_words(m):
+@pytest.mark.parametrize("dtype,heads,hd", SHAPES)
+@pytest.mark.parametrize("i", range(len(LENS)))
+@pytest.mark.parametrize("kind,group", [("none", 1), ("tree", 1), ("tree", 3), ("causal", 8), ("empty", 2)])
+def test_attend(m, dtype, heads, hd, i, kind, group):
+    attend_case(m, dtype, heads, hd, i, kind, group)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("i,kind,group", [(0, "tree", 3), (3, "causal", 8), (4, "empty", 9), (5, "tree", 5)])
+def test_attend_much_work(m, hd, i, kind, group):
+    """Many cache heads and page-table rows of 32768 positions: what a call has to do at most chooses the form of many rows."""
+    attend_case(m, "bf16", 20, hd, i, kind, group, columns=2048)
+
+
+@pytest.mark.parametrize("columns", [0, 2048])
+def test_attend_long_runs_without_words(m, columns):
     torch = m.torch
-    c = m.Cache("bf16", 2, 64, [300, 65], [70, 0], seed=5)
-    q = c.randn(c.T, 256)
-    out, lse = torch.empty_like(q), torch.empty(c.T, 4, device=m.DEV)
+    heads = 8 if columns else 2
+    c = m.Cache("bf16", heads, 64, [300, 65], [70, 0], seed=5, columns=columns)
+    q = c.randn(c.T, heads * 2 * 64)
+    out, lse = torch.empty_like(q), torch.empty(c.T, heads * 2, device=m.DEV)
     c.ctx.attend(0, c.lens, c.d_past, c.d_table, q, out, lse=lse)
     m.check_attention(c, q, 2, out, lse)
     c.close()
 
 
-@pytest.mark.parametrize("dtype,heads,hd", SHAPES)
-@pytest.mark.parametrize("past", [0, 37, 900])
-@pytest.mark.parametrize("group", [1, 2, 3, 9])
-def test_attend_what_is_hidden_does_not_reach(m, dtype, heads, hd, past, group):
-    """NaN and infinities in new keys and values that a token does not see, and behind the last key; those it sees do reach it.
-    (The groups choose the forms: 30, 60, 90 and 270 rows per cache head.)"""
+def hidden_case(m, dtype, heads, hd, past, group, columns=0):
     torch = m.torch
     n = 30
-    c = m.Cache(dtype, heads, hd, [n, 9], [past, 3], seed=7)
+    c = m.Cache(dtype, heads, hd, [n, 9], [past, 3], seed=7, columns=columns)
     bad = [3, 11, 12, 29]
     kv = torch.randn(4, heads, hd, generator=c.g)
     kv[0], kv[1, :, ::3], kv[2, :, 1::2], kv[3] = math.nan, math.inf, -math.inf, math.nan
@@ -236,6 +244,23 @@ def test_attend_what_is_hidden_does_not_reach(m, dtype, heads, hd, past, group):
     c.ctx.attend(0, c.lens, c.d_past, c.d_table, q, out, visible=m.word_tensor(words), lse=lse)
     assert torch.isnan(out[8]).all() and torch.isnan(lse[8]).all() and torch.isfinite(out[9:]).all()
     c.close()
+
+
+@pytest.mark.parametrize("dtype,heads,hd", SHAPES)
+@pytest.mark.parametrize("past", [0, 37, 900])
+@pytest.mark.parametrize("group", [1, 2, 3, 9])
+def test_attend_what_is_hidden_does_not_reach(m, dtype, heads, hd, past, group):
+    """NaN and infinities in new keys and values that a token does not see, and behind the last key; those it sees do reach it.
+    (The groups choose the forms: 30, 60, 90 and 270 rows per cache head.)"""
+    hidden_case(m, dtype, heads, hd, past, group)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("past", [0, 37, 900])
+@pytest.mark.parametrize("group", [3, 9])
+def test_attend_what_is_hidden_does_not_reach_much_work(m, hd, past, group):
+    """The same in the form of many rows, of 90 rows and of 270."""
+    hidden_case(m, "bf16", 20, hd, past, group, columns=2048)
 
 
 def test_attend_extreme_scores(m):
