@@ -30,7 +30,8 @@ class Cache:
         self.free = order[at:]
         cfg = di.configs.scaled(di.model_preset("tiny"), n_layers=layers, hidden=64, n_heads=heads, head_dim=head_dim, n_experts=1, top_k=1,
                                 moe_inter=64, vocab=64, dtype=dtype)
-        self.ctx = binding.Context(cfg, self.n_pages, self.ns, 64, max_pos or max(need + [columns]) * PAGE)
+        self.cfg, self.max_pos = cfg, max_pos or max(need + [columns]) * PAGE
+        self.ctx = binding.Context(cfg, self.n_pages, self.ns, 64, self.max_pos)
         self.pool = self.ctx.kv.view(TYPE[dtype]).view(layers, self.n_pages, 2, -1)
         self.pool.copy_(torch.randn(self.pool.shape, generator=g).to(TYPE[dtype]))
         self.d_table, self.d_past = self.table.to(DEV), torch.tensor(past, dtype=torch.int32, device=DEV)

@@ -242,6 +242,32 @@ def test_two_contexts_on_two_streams(m):
         c.close()
 
 
+def test_pages_beyond_32_bits(m):
+    """The same rows in pages whose elements are numbered from 2^32 on (a pool of 8 GiB and more): the same outputs and pages."""
+    import copy
+    import torch
+    c, b, words = layer_case(m)
+    far, fb = copy.copy(c), dict(b)
+    first = 2 ** 32 // (2 * 4 * 64 * 16)                  # elements of a page
+    far.ctx = m.binding.Context(c.cfg, first + c.n_pages, c.ns, 64, c.max_pos)
+    pool = far.ctx.kv.view(torch.bfloat16).view(first + c.n_pages, -1)[first:]
+    pool.copy_(c.pool.view(c.n_pages, -1))
+    low = far.ctx.kv.view(torch.bfloat16).view(first + c.n_pages, -1)[:c.n_pages]
+    low.zero_()
+    far.d_table = torch.where(c.d_table >= 0, c.d_table + first, c.d_table)
+    fb["new_table"] = b["new_table"] + first
+    for n in OUTS:
+        fb[n] = torch.zeros_like(b[n])
+    layer_run(m, c, b, words)
+    layer_run(m, far, fb, words)
+    torch.cuda.synchronize()
+    for n in OUTS:
+        assert torch.equal(b[n], fb[n]), n
+    assert torch.equal(pool.view(torch.int16), c.pool.view(c.n_pages, -1).view(torch.int16)) and (low == 0).all()
+    far.close()
+    c.close()
+
+
 def test_refusals(m):
     """Bad arguments are refused before anything is launched: every output keeps what it held."""
     import torch
