@@ -315,7 +315,8 @@ int dinfer_kv_read(dinfer_ctx* ctx, int32_t layer, const int32_t* d_page_row, in
  * between rows) are multiples of 16 bytes.  n_q_heads: query heads, a multiple of the configuration's n_heads; query head i
  * belongs to cache head i / (n_q_heads / n_heads).  `layer` chooses the part of the pool.  The context must be used
  * with the GPU that was current at dinfer_create (DINFER_EINVAL otherwise).  Sums, statistics and angles are float32 or
- * wider; outputs are rounded once. */
+ * wider; outputs are rounded once.  (Attention weights of a bfloat16 cache enter the product with the values as two bfloat16
+ * numbers each, which are within 2^-15 of the weight together.) */
 
 /* A rotation of the first rotary_dim features of a head (even, at most head_dim; the others pass through): pairs
  * (j, j + rotary_dim/2), or (2j, 2j+1) with interleaved != 0, turn by position * f_j, f_j = theta^(-2j/rotary_dim) changed by

@@ -4,9 +4,7 @@
 // The queries of all query heads that share a cache head are rows of the same contraction (row = token * group + member), so
 // that a tile of 32 rows reads its head's keys once.  MFMA mapping as in attention.hip: S^T[key][row] = K . Q^T, a lane owns
 // one row, O^T[d][row] += V^T . P^T from the score registers.  Queries enter as they are (bfloat16 queries are exact), and
-// probabilities as one bfloat16 plane: a rounding is off by at most 2^-8 of a probability, they fall either way, and an output is their
-// mean over the keys (error against 64 bits 0.0022 of the outputs, 0.0017 with 32-bit probabilities and the same rounded outputs).  Sums
-// of probabilities are those of the unrounded ones.
+// probabilities as two bfloat16 planes (PvWeights), so that an output is rounded once, when it is stored.
 #include <type_traits>
 
 #include "attn_tiles.hpp"
@@ -87,6 +85,34 @@ __device__ inline void take_scores(const f32x16 (&s)[NS], float c2, float& m_run
     }
   l_run += sum;
 }
+
+// Probabilities of k-step s2 as operands of the product with V.  bfloat16: a plane of the leading eight bits, cut off, and a plane of the
+// rest, which is off by 2^-15 of the probability at most.  The rest is never negative, and one step of float32 more than it is, so that it is
+// not zero next to a probability that is not: an infinite value times both planes is the infinity.
+template <typename E> struct PvWeights;
+template <> struct PvWeights<bf16_t> {
+  static constexpr int PLANES = 2;
+  __device__ static void pair(const float (&p)[16], int s2, int j, u32x4 (&w)[2]) {
+    constexpr float STEP = 1.f + 0x1p-23f;
+    const float a = p[8 * s2 + 2 * j], b = p[8 * s2 + 2 * j + 1];
+    const uint32_t ua = __float_as_uint(a), ub = __float_as_uint(b);
+    typedef bf16_t bf16x2 __attribute__((ext_vector_type(2)));
+    w[0][j] = __builtin_amdgcn_perm(ub, ua, 0x07060302u);      // their upper halves
+    w[1][j] = __builtin_bit_cast(uint32_t, bf16x2{(bf16_t)fmaf(a, STEP, -__uint_as_float(ua & 0xffff0000u)),
+                                                  (bf16_t)fmaf(b, STEP, -__uint_as_float(ub & 0xffff0000u))});
+  }
+  __device__ static void split(const float (&p)[16], int s2, bf16x8 (&w)[2]) {
+    u32x4 x[2];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) pair(p, s2, j, x);
+    w[0] = __builtin_bit_cast(bf16x8, x[0]);
+    w[1] = __builtin_bit_cast(bf16x8, x[1]);
+  }
+};
+template <> struct PvWeights<float> {
+  static constexpr int PLANES = 1;
+  __device__ static void split(const float (&p)[16], int s2, f32x4 (&w)[1]) { w[0] = PvStep<float>::p_vec(p, s2, 0); }
+};
 
 // Weight of a partial state (m, l) against the maximum M of all: a state that saw nothing counts nothing, one that is not a
 // number (every score NaN: m never moved) makes the sum one.
@@ -342,9 +368,10 @@ __global__ __launch_bounds__(ATTEND_WAVES * WAVE, (attend_waves_per_simd<E, HD>(
     float p[1][16];
     take_scores<DT, 1>(s, c2, m_run, l_run, o, p);
     if constexpr (PV) {
-      vec pv[STEPS];
+      constexpr int PP = PvWeights<E>::PLANES;
+      vec pv[STEPS][PP];
 #pragma unroll
-      for (int s2 = 0; s2 < STEPS; ++s2) pv[s2] = PvStep<E>::p_vec(p[0], s2, 0);
+      for (int s2 = 0; s2 < STEPS; ++s2) PvWeights<E>::split(p[0], s2, pv[s2]);
       if (decltype(tail)::value && odd) {
         // 0 * NaN would reach the rows that do not see the key: the product takes 0 in such a value's place, and the rows with
         // weight on it are found by products with its indicator, one kind (NaN, +inf, -inf) at a time, and marked
@@ -369,7 +396,7 @@ __global__ __launch_bounds__(ATTEND_WAVES * WAVE, (attend_waves_per_simd<E, HD>(
 #pragma unroll
             for (int s2 = 0; s2 < STEPS; ++s2) {
               const vec x = PvStep<E>::v_vec(v_row(kt, s2) + t * (TILE * PAGE), half, s2);
-              mfma32(hit[0], odd_values<E>(x, kind, n_keys - (kt * TILE + PvStep<E>::key_of(s2, half, 0))), pv[s2]);
+              mfma32(hit[0], odd_values<E>(x, kind, n_keys - (kt * TILE + PvStep<E>::key_of(s2, half, 0))), pv[s2][0]);
             }
             uint32_t bits = 0;
 #pragma unroll
@@ -380,7 +407,9 @@ __global__ __launch_bounds__(ATTEND_WAVES * WAVE, (attend_waves_per_simd<E, HD>(
 #pragma unroll
       for (int s2 = 0; s2 < STEPS; ++s2)
 #pragma unroll
-        for (int t = 0; t < DT; ++t) mfma32(o[t], v[s2][t], pv[s2]);
+        for (int pl = 0; pl < PP; ++pl)
+#pragma unroll
+          for (int t = 0; t < DT; ++t) mfma32(o[t], v[s2][t], pv[s2][pl]);
       __builtin_amdgcn_sched_barrier(0);
       load_v(next);
     }
@@ -609,16 +638,24 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void attend_rows_kernel(AttendArgs
           marks[kind] |= (uint64_t)bits << (16 * t);
         }
     }
+    // (a step's weights are split between the products of the step in front of it)
+    u32x4 pv[2][2];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) PvWeights<E>::pair(p[0], 0, j, pv[0]);
 #pragma unroll
     for (int u = 0; u < 2 * STEPS; ++u) {
-      const vec pv = PvStep<E>::p_vec(p[u / STEPS], u % STEPS, 0);
 #pragma unroll
       for (int t = 0; t < DT; ++t) {
         const int f = u * DT + t;
         const vec v = ring[f % RD];
         if (f + RD < NF) ring[f % RD] = tiles[2 + (f + RD) / WF][(f + RD) % WF][lane];
         __builtin_amdgcn_sched_barrier(0);
-        mfma32(o[t], v, pv);
+        mfma32(o[t], v, __builtin_bit_cast(vec, pv[u & 1][0]));
+        if (u + 1 < 2 * STEPS) {
+#pragma unroll
+          for (int j = t * 4 / DT; j < (t + 1) * 4 / DT; ++j) PvWeights<E>::pair(p[(u + 1) / STEPS], (u + 1) % STEPS, j, pv[(u + 1) & 1]);
+        }
+        mfma32(o[t], v, __builtin_bit_cast(vec, pv[u & 1][1]));
       }
     }
   };
@@ -780,12 +817,13 @@ static int64_t most_meetings(const AttendArgs& a) {
   return row_tiles * a.geom.n_heads * ((a.tok.limit + TILE - 1) / TILE);
 }
 // Two row tiles per workgroup where a sequence has more than one; more than two: the form whose tiles go through LDS, where there is
-// work enough for it.  Its workgroups are few and take 2.4 us a turn, however little there is: of 8 cache heads of 4 queries each, 60
-// tokens behind 3000 positions take 37.0 us in it and 19.0 in two row tiles, four sequences of them (24 thousand meetings) 45.0
-// and 34.6, eight (49 thousand) 58.8 and 62.0, sixteen 87 and 101; 20, 24 and 16 tokens, 16 and 4 heads and 8 queries per head cross over
-// between 40 and 70 thousand as well.  In float32 the matrix instructions are the bound (a sixteenth of the rate), not the reads that row
+// work enough for it.  Its workgroups are few and take 3 us a turn, however little there is: of 8 cache heads of 4 queries each, 60
+// tokens behind 3000 positions take 38.8 us in it and 20.3 in two row tiles, eight sequences of them (49 thousand meetings) 65 and 63,
+// sixteen 98 and 92, 24 (148 thousand) 178 and 153, 32 163 and 202, 48 278 and 298.  How a call's parts fill its 256 places moves the
+// crossover: 16 heads of 8 queries and 20 tokens 151 and 133 at 91 thousand, 138 and 154 at 121, 4 heads of 8 and 64 tokens 91 and 95 at 97,
+// 183 and 139 at 145, 156 and 165 at 194.  In float32 the matrix instructions are the bound (a sixteenth of the rate), not the reads that row
 // tiles could share: one tile per workgroup (3 sequences of 5 to 33 tokens 28.9 -> 20.4 us).
-constexpr int64_t ROWS_FORM_MEETINGS = 1 << 16;
+constexpr int64_t ROWS_FORM_MEETINGS = 1 << 17;
 template <int HD> static void launch_attend_hd(bool bf16, int planes, const AttendArgs& a, hipStream_t st) {
   const int most = most_rows(a.tok.span, a.group);
   if (bf16) {
