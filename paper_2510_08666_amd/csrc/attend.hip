@@ -659,10 +659,12 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void attend_rows_kernel(AttendArgs
       }
     }
   };
-  // The turns in front of the tail, and the one before it, whose neighbour has to be masked on its way to LDS.
+  // The turns in front of the tail, and the one before it, whose neighbour has to be masked on its way to LDS.  A turn that was put as one
+  // of the tail is taken as one, so that what was replaced on its way is looked for.
   const int full = (min(c.base, last_key + 1) - kt0 * TILE) / (2 * TILE);
   fetch(0);
-  put(0, std::true_type{});
+  if (full > 1) put(0, std::false_type{});
+  else put(0, std::true_type{});
   fetch(1);
   int turn = 0;
   for (; turn + 1 < full; ++turn) {
