@@ -361,7 +361,9 @@ int dinfer_kv_append(dinfer_ctx* ctx, int32_t layer, int32_t n_seq, const int32_
  *              see, infinities and NaN included, does not reach it.  A token that sees nothing gets zeros.
  *   scale      of the scores; 0: 1/sqrt(head_dim).
  *   d_out      [T] rows of n_q_heads heads.
- *   d_lse      [T][n_q_heads] float32, or null: logarithm of every row's sum of exponentials (-infinity: sees nothing). */
+ *   d_lse      [T][n_q_heads] float32, or null: logarithm of every row's sum of exponentials (-infinity: sees nothing).
+ * One call takes fewer than 2^31 meetings of 32 rows with 32 positions, counted as if every cache were full (DINFER_EUNSUPPORTED):
+ *   (ceil(T * group / 32) + n_seq) * n_heads * ceil(P / 32), group = n_q_heads / n_heads, P = min(max_pos, 16 * pt_stride). */
 int dinfer_attend(dinfer_ctx* ctx, int32_t layer, int32_t n_seq, const int32_t* h_lens, const int32_t* d_past,
                   const int32_t* d_page_table, int32_t pt_stride, const void* d_q, int64_t q_stride, int32_t n_q_heads,
                   const uint64_t* d_visible, float scale, void* d_out, int64_t out_stride, float* d_lse, void* stream);
@@ -371,7 +373,7 @@ int dinfer_attend(dinfer_ctx* ctx, int32_t layer, int32_t n_seq, const int32_t* 
  * the head's query heads.  d_score_in null: 0; it may be d_score_out.  Both [n_seq][n_heads][score_stride] float32; other
  * entries, and sequences without new tokens, are left alone.
  *   d_lse      [T][n_q_heads] float32: with lse_given != 0 what dinfer_attend left for the same arguments; with 0 it is worked
- *              out first (one more pass over the keys) and left there.
+ *              out first (one more pass over the keys, of the size that dinfer_attend takes) and left there.
  * Every entry has one writer and a fixed order of additions: the same bits every time. */
 int dinfer_kv_score(dinfer_ctx* ctx, int32_t layer, int32_t n_seq, const int32_t* h_lens, const int32_t* d_past,
                     const int32_t* d_page_table, int32_t pt_stride, const void* d_q, int64_t q_stride, int32_t n_q_heads,

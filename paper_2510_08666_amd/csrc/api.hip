@@ -1026,10 +1026,14 @@ static int cache_tokens(dinfer_ctx* c, int32_t layer, int32_t n_seq, const int32
       return fail(DINFER_ENOSPACE, "%d new tokens exceed max_pos %d or the page-table row (%d pages)", h_lens[s], c->cfg.max_pos, pt_stride);
     tok->span.off[s + 1] = tok->span.off[s] + h_lens[s];     // <= 64 * 32768
   }
-  // what the kernels number their work by: key tiles of every 32 rows of every cache head
-  const int64_t row_tiles = ((int64_t)tok->span.off[n_seq] * (n_q_heads / c->cfg.n_heads) + TILE - 1) / TILE + n_seq;
-  if (row_tiles * c->cfg.n_heads * ((tok->limit + TILE - 1) / TILE) > INT32_MAX)
-    return fail(DINFER_EUNSUPPORTED, "%d new tokens of %d heads over %d positions are too many for one call", tok->span.off[n_seq], n_q_heads, tok->limit);
+  return DINFER_OK;
+}
+// What attention's kernels number their work by: key tiles of every 32 rows of every cache head.
+static int check_meetings(const dinfer_ctx* c, const CacheTokens& tok, int32_t n_q_heads) {
+  const int T = tok.span.off[tok.span.n_seq];
+  const int64_t row_tiles = ((int64_t)T * (n_q_heads / c->cfg.n_heads) + TILE - 1) / TILE + tok.span.n_seq;
+  if (row_tiles * c->cfg.n_heads * ((tok.limit + TILE - 1) / TILE) > INT32_MAX)
+    return fail(DINFER_EUNSUPPORTED, "%d new tokens of %d heads over %d positions are too many for one call", T, n_q_heads, tok.limit);
   return DINFER_OK;
 }
 static int check_device(const dinfer_ctx* c) {
@@ -1165,6 +1169,7 @@ int dinfer_attend(dinfer_ctx* c, int32_t layer, int32_t n_seq, const int32_t* h_
   if (rc != DINFER_OK) return rc;
   if ((rc = check_rows(c, "d_q", d_q, q_stride, n_q_heads)) != DINFER_OK) return rc;
   if ((rc = check_rows(c, "d_out", d_out, out_stride, n_q_heads)) != DINFER_OK) return rc;
+  if ((rc = check_meetings(c, a.tok, n_q_heads)) != DINFER_OK) return rc;
   if ((rc = check_visible(a.tok, d_visible)) != DINFER_OK) return rc;
   if ((rc = check_scale(c, scale, &a.scale)) != DINFER_OK) return rc;
   if ((rc = check_device(c)) != DINFER_OK) return rc;
@@ -1191,6 +1196,7 @@ int dinfer_kv_score(dinfer_ctx* c, int32_t layer, int32_t n_seq, const int32_t* 
   if (rc != DINFER_OK) return rc;
   if ((rc = check_rows(c, "d_q", d_q, q_stride, n_q_heads)) != DINFER_OK) return rc;
   if (!d_lse || !d_score_out) return fail(DINFER_EINVAL, "null pointer");
+  if (!lse_given && (rc = check_meetings(c, a.tok, n_q_heads)) != DINFER_OK) return rc;
   if (score_stride < 1) return fail(DINFER_EINVAL, "score_stride %d", score_stride);
   if (!(decay >= 0.f && decay < INFINITY)) return fail(DINFER_EINVAL, "decay %g", (double)decay);
   if ((rc = check_visible(a.tok, d_visible)) != DINFER_OK) return rc;
