@@ -68,7 +68,7 @@ class SmoothSchedule(ctypes.Structure):
 
 class Rotary(ctypes.Structure):
     _fields_ = [(n, c_i32) for n in ("rotary_dim", "interleaved", "scaling", "original_positions")] + \
-               [(n, c_f32) for n in ("theta", "factor", "beta_fast", "beta_slow", "magnitude")]
+               [(n, ctypes.c_double) for n in ("theta", "factor", "beta_fast", "beta_slow", "magnitude")]
 
 
 class CacheUse(ctypes.Structure):

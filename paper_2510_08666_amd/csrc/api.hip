@@ -1,6 +1,7 @@
 // C-ABI of the dinfer library: argument checks, buffer carving, and the launch sequence of one forward.
 #include "../../include/dinfer.h"
 
+#include <float.h>
 #include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
@@ -1067,25 +1068,26 @@ static int rotary_rule(const dinfer_rotary* r, RotaryRule* out) {
   if (!r) return fail(DINFER_EINVAL, "rotary is null");
   if (r->rotary_dim < 2 || r->rotary_dim % 2 || r->rotary_dim > 128) return fail(DINFER_EINVAL, "rotary_dim %d", r->rotary_dim);
   if (r->scaling < DINFER_ROTARY_PLAIN || r->scaling > DINFER_ROTARY_YARN) return fail(DINFER_EINVAL, "scaling %d", r->scaling);
-  if (!(r->theta > 0.f && r->theta < INFINITY)) return fail(DINFER_EINVAL, "theta %g", (double)r->theta);
-  if (r->scaling != DINFER_ROTARY_PLAIN && !(r->factor > 0.f && r->factor < INFINITY)) return fail(DINFER_EINVAL, "factor %g", (double)r->factor);
+  // (float32's range: no angle that follows leaves double's)
+  if (!(r->theta >= FLT_MIN && r->theta <= FLT_MAX)) return fail(DINFER_EINVAL, "theta %g", r->theta);
+  if (r->scaling != DINFER_ROTARY_PLAIN && !(r->factor >= FLT_MIN && r->factor <= FLT_MAX)) return fail(DINFER_EINVAL, "factor %g", r->factor);
   const double n = r->rotary_dim;
   *out = RotaryRule{r->rotary_dim, r->scaling, r->theta, r->factor, 0.0, 1.0, 1.0};
   if (r->scaling == DINFER_ROTARY_NTK) {
     if (r->rotary_dim == 2) return fail(DINFER_EINVAL, "a raised base needs rotary_dim > 2");
-    out->theta = r->theta * pow((double)r->factor, n / (n - 2));
+    out->theta = r->theta * pow(r->factor, n / (n - 2));
   }
   if (r->scaling == DINFER_ROTARY_YARN) {
-    const double fast = r->beta_fast == 0.f ? 32.0 : r->beta_fast, slow = r->beta_slow == 0.f ? 1.0 : r->beta_slow;
-    if (!(fast >= slow && slow > 0.0 && fast < INFINITY) || r->original_positions < 1 || !(r->theta > 1.f) || !(r->magnitude >= 0.f && r->magnitude < INFINITY))
+    const double fast = r->beta_fast == 0 ? 32.0 : r->beta_fast, slow = r->beta_slow == 0 ? 1.0 : r->beta_slow;
+    if (!(fast >= slow && slow > 0.0 && fast < INFINITY) || r->original_positions < 1 || !(r->theta > 1.0) || !(r->magnitude >= 0.0 && r->magnitude <= FLT_MAX))
       return fail(DINFER_EINVAL, "ramped frequencies: beta_fast >= beta_slow > 0, original_positions >= 1, theta > 1, magnitude >= 0");
     const double two_pi = 6.283185307179586476925286766559;
-    const double lo = floor(n * log(r->original_positions / (fast * two_pi)) / (2 * log((double)r->theta)));
-    const double hi = ceil(n * log(r->original_positions / (slow * two_pi)) / (2 * log((double)r->theta)));
+    const double lo = floor(n * log(r->original_positions / (fast * two_pi)) / (2 * log(r->theta)));
+    const double hi = ceil(n * log(r->original_positions / (slow * two_pi)) / (2 * log(r->theta)));
     out->low = lo > 0 ? lo : 0;
     out->high = hi < n - 1 ? hi : n - 1;
     if (out->high - out->low < 0.001) out->high = out->low + 0.001;
-    out->magnitude = r->magnitude > 0.f ? r->magnitude : 0.1 * log((double)r->factor) + 1.0;
+    out->magnitude = r->magnitude > 0 ? r->magnitude : 0.1 * log(r->factor) + 1.0;
   }
   return DINFER_OK;
 }

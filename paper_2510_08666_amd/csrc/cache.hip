@@ -5,8 +5,8 @@
 namespace dinfer {
 
 // ---------------------------------------------------------------- rotary tables
-// cos / sin of pos * f_j times the rule's magnitude, worked out in double and stored as float: a float32 angle of position
-// 32767 is off by up to 2e-3.
+// cos / sin of pos * f_j times the rule's magnitude, worked out in double from a rule in double and stored as float: a float32 angle of
+// position 32767 is off by up to 2e-3, and a base or factor that was rounded to float32 turns it as far.
 __global__ __launch_bounds__(256) void rotary_table_kernel(RotaryRule r, int max_pos, float* __restrict__ cos_tab, float* __restrict__ sin_tab) {
   const int half = r.rotary_dim / 2;
   const int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;

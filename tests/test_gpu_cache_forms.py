@@ -38,3 +38,47 @@ def test_append_of_more_tokens_than_one_attention_call_takes(m):
     for s in range(ns):
         assert torch.equal(q[s * n:(s + 1) * n], out[s * n:(s + 1) * n]), s
     c.close()
+
+
+def angles(r, n, scaling, theta, factor, original, fast, slow, magnitude):
+    """Cosines and sines of positions 0 .. n-1 in float64."""
+    import torch
+    j = torch.arange(r // 2, dtype=torch.float64)
+    f = (theta * factor ** (r / (r - 2)) if scaling == "ntk" else theta) ** (-2 * j / r)
+    size = 1.0
+    if scaling == "linear":
+        f = f / factor
+    if scaling == "yarn":
+        corner = [r * math.log(original / (b * 2 * math.pi)) / (2 * math.log(theta)) for b in (fast, slow)]
+        lo, hi = max(0, math.floor(corner[0])), min(r - 1, math.ceil(corner[1]))
+        ramp = ((j - lo) / max(hi - lo, 0.001)).clamp(0, 1)
+        f = f * (1 - ramp) + f / factor * ramp
+        size = magnitude or 0.1 * math.log(factor) + 1
+    a = torch.arange(n, dtype=torch.float64)[:, None] * f
+    return torch.stack([a.cos(), a.sin()]) * size
+
+
+def check_table(m, r, n, scaling, theta, factor, original=0, fast=32.0, slow=1.0, magnitude=0.0, set_betas=True):
+    """Within half a step of float32 and what double leaves of an angle of 32767 (a few steps of 2^-52)."""
+    import torch
+    rot = m.binding.rotary(r, False, theta, scaling, factor, original, fast if set_betas else 0.0, slow if set_betas else 0.0, magnitude)
+    got = m.binding.rotary_table(rot, n).cpu().double()
+    ref = angles(r, n, scaling, theta, factor, original, fast, slow, magnitude)
+    assert got.shape == ref.shape
+    d = (got - ref).abs()
+    assert (d <= 2.0 ** -24 * ref.abs() + 1e-9).all(), float(d.max())
+
+
+@pytest.mark.parametrize("scaling,factor", [("plain", 1.0), ("linear", 3.3), ("ntk", 1.7), ("yarn", 3.3)])
+@pytest.mark.parametrize("theta", [10000.0, 12345.67])
+def test_rotary_rules_that_float32_cannot_hold(m, scaling, factor, theta):
+    check_table(m, 64, 32768, scaling, theta, factor, 2048)
+
+
+@pytest.mark.parametrize("r", [20, 64, 128])
+@pytest.mark.parametrize("original,fast,slow,magnitude", [(2048, 32.0, 1.0, 0.0), (4096, 16.0, 2.5, 0.0), (300, 4.0, 4.0, 1.3), (8192, 100.0, 0.25, 0.7)])
+def test_ramped_frequencies(m, r, original, fast, slow, magnitude):
+    """The ramp's corners from other numbers of turns than 32 and 1, and a magnitude of one's own."""
+    check_table(m, r, 5000, "yarn", 10000.0, 4.0, original, fast, slow, magnitude)
+    if (fast, slow) == (32.0, 1.0):
+        check_table(m, r, 5000, "yarn", 10000.0, 4.0, original, fast, slow, magnitude, set_betas=False)
