@@ -326,7 +326,7 @@ int dinfer_kv_read(dinfer_ctx* ctx, int32_t layer, const int32_t* d_page_row, in
  *   DINFER_ROTARY_YARN    f_j for pairs that turn often within original_positions, f_j / factor for those that hardly turn, a linear ramp in j
  *                         between: from low = floor(c(beta_fast)) (at least 0) to high = ceil(c(beta_slow)) (at most r - 1),
  *                         c(b) = r ln(original_positions / (2 pi b)) / (2 ln theta); cosines and sines times magnitude
- *                         (0: 0.1 ln(factor) + 1; 1 for the other kinds).
+ *                         (0: 0.1 ln(factor) + 1 for factor > 1, else 1; 1 for the other kinds).
  * beta_fast and beta_slow 0: 32 and 1.  theta and factor are positive and within float32's range. */
 enum { DINFER_ROTARY_PLAIN = 0, DINFER_ROTARY_LINEAR = 1, DINFER_ROTARY_NTK = 2, DINFER_ROTARY_YARN = 3 };
 typedef struct {

@@ -1087,7 +1087,7 @@ static int rotary_rule(const dinfer_rotary* r, RotaryRule* out) {
     out->low = lo > 0 ? lo : 0;
     out->high = hi < n - 1 ? hi : n - 1;
     if (out->high - out->low < 0.001) out->high = out->low + 0.001;
-    out->magnitude = r->magnitude > 0 ? r->magnitude : 0.1 * log(r->factor) + 1.0;
+    out->magnitude = r->magnitude > 0 ? r->magnitude : r->factor > 1.0 ? 0.1 * log(r->factor) + 1.0 : 1.0;
   }
   return DINFER_OK;
 }

@@ -53,7 +53,7 @@ def angles(r, n, scaling, theta, factor, original, fast, slow, magnitude):
         lo, hi = max(0, math.floor(corner[0])), min(r - 1, math.ceil(corner[1]))
         ramp = ((j - lo) / max(hi - lo, 0.001)).clamp(0, 1)
         f = f * (1 - ramp) + f / factor * ramp
-        size = magnitude or 0.1 * math.log(factor) + 1
+        size = magnitude or (0.1 * math.log(factor) + 1 if factor > 1 else 1.0)
     a = torch.arange(n, dtype=torch.float64)[:, None] * f
     return torch.stack([a.cos(), a.sin()]) * size
 
@@ -82,3 +82,9 @@ def test_ramped_frequencies(m, r, original, fast, slow, magnitude):
     check_table(m, r, 5000, "yarn", 10000.0, 4.0, original, fast, slow, magnitude)
     if (fast, slow) == (32.0, 1.0):
         check_table(m, r, 5000, "yarn", 10000.0, 4.0, original, fast, slow, magnitude, set_betas=False)
+
+
+@pytest.mark.parametrize("factor", [1.0, 0.5, 1e-6])
+def test_ramped_frequencies_that_do_not_stretch(m, factor):
+    """A factor of at most one leaves cosines and sines their size."""
+    check_table(m, 64, 300, "yarn", 10000.0, factor, 2048)
