@@ -425,11 +425,18 @@ class Context:
     def _rows(self, name, t, rows, heads):
         """Address and stride of a matrix of at least `rows` rows of heads * head_dim contiguous elements."""
         width = heads * self.cfg.head_dim
-        if t.dtype is self._dtype and t.dim() == 2 and t.get_device() == self._index:
+        if t is not None and t.dtype is self._dtype and t.dim() == 2 and t.get_device() == self._index:
             (n, m), (stride, one) = t.shape, t.stride()
             if n >= rows and m == width and one == 1:
                 return t.data_ptr(), stride
         raise ValueError("%s must be a [%d][%d] tensor of the context's dtype and device, rows contiguous" % (name, rows, width))
+
+    @staticmethod
+    def _sizes(name, t, dims):
+        """Sizes of a tensor that has `dims` of them."""
+        if t is None or t.dim() != dims:
+            raise ValueError("%s must be a tensor of %d dimensions" % (name, dims))
+        return t.shape
 
     def _flat(self, name, t, dtype, *shape):
         """Address of a contiguous tensor of that type and these sizes (the first may be larger); None passes."""
@@ -443,9 +450,9 @@ class Context:
 
     def _tokens(self, lens, d_past, d_page_table):
         """The arguments that say which tokens join which sequences, and how many there are."""
-        n = len(lens)
+        n, columns = len(lens), self._sizes("d_page_table", d_page_table, 2)[1]
         return ((n, (c_i32 * n)(*lens), self._flat("d_past", d_past, torch.int32, n),
-                 self._flat("d_page_table", d_page_table, torch.int32, n, d_page_table.shape[1]), d_page_table.shape[1]), sum(lens))
+                 self._flat("d_page_table", d_page_table, torch.int32, n, columns), columns), sum(lens))
 
     def _words(self, visible, T):
         if visible is not None and visible.dtype is torch.uint64:
@@ -457,11 +464,11 @@ class Context:
         """Norms, rotates and stores a layer's new tokens; d_q_out receives the queries (d_q and d_q_out None: keys and values only)."""
         tok, T = self._tokens(lens, d_past, d_page_table)
         nh, hd = self.cfg.n_heads, self.cfg.head_dim
-        nq = nh if d_q is None else d_q.shape[1] // hd
+        nq = nh if d_q is None else self._sizes("d_q", d_q, 2)[1] // hd
         q, out = ((None, 0), (None, 0)) if d_q is None else (self._rows("d_q", d_q, T, nq), self._rows("d_q_out", d_q_out, T, nq))
         table_positions = 0
         if rotary is not None and rotary_table is not None:
-            table_positions = rotary_table.shape[1]
+            table_positions = self._sizes("rotary_table", rotary_table, 3)[1]
             self._flat("rotary_table", rotary_table, torch.float32, 2, table_positions, rotary.rotary_dim // 2)
         _check(lib.dinfer_kv_append(self.h, layer, *tok, *q, *self._rows("d_k", d_k, T, nh), *self._rows("d_v", d_v, T, nh), nq,
                                     self._flat("q_gain", q_gain, torch.float32, hd), self._flat("k_gain", k_gain, torch.float32, hd), eps,
@@ -471,7 +478,7 @@ class Context:
     def attend(self, layer, lens, d_past, d_page_table, d_q, d_out, visible=None, scale=0.0, lse=None):
         """Attention of the new tokens over the cache, their own keys as far as the words of `visible` [T] allow."""
         tok, T = self._tokens(lens, d_past, d_page_table)
-        nq = d_q.shape[1] // self.cfg.head_dim
+        nq = self._sizes("d_q", d_q, 2)[1] // self.cfg.head_dim
         _check(lib.dinfer_attend(self.h, layer, *tok, *self._rows("d_q", d_q, T, nq), nq, self._words(visible, T), scale,
                                  *self._rows("d_out", d_out, T, nq), self._flat("lse", lse, torch.float32, T, nq), self._raw_stream()))
 
@@ -480,7 +487,8 @@ class Context:
         """Adds the attention weight of the new tokens to d_score_out [n_seq][n_heads][stride]; lse: what `attend` left for
         the same queries (None: worked out here)."""
         tok, T = self._tokens(lens, d_past, d_page_table)
-        nq, shape = d_q.shape[1] // self.cfg.head_dim, (len(lens), self.cfg.n_heads, d_score_out.shape[2])
+        nq = self._sizes("d_q", d_q, 2)[1] // self.cfg.head_dim
+        shape = (len(lens), self.cfg.n_heads, self._sizes("d_score_out", d_score_out, 3)[2])
         q = self._rows("d_q", d_q, T, nq)
         given = lse is not None
         if not given:
@@ -492,18 +500,18 @@ class Context:
     def kv_evict(self, first_layer, n_layers, keep, n_sink, n_recent, d_score, d_len, d_page_table, d_new_page_table, d_kept,
                  d_new_len, score_out=None):
         """Keeps `keep` positions per (layer, sequence, head) of d_score [n_layers][n_seq][n_heads][stride] in new pages."""
-        ns, nh, width = d_page_table.shape[0], self.cfg.n_heads, d_score.shape[3]
-        i32 = torch.int32
+        (ns, columns), (_, new_columns) = self._sizes("d_page_table", d_page_table, 2), self._sizes("d_new_page_table", d_new_page_table, 2)
+        nh, width, i32 = self.cfg.n_heads, self._sizes("d_score", d_score, 4)[3], torch.int32
         _check(lib.dinfer_kv_evict(self.h, first_layer, n_layers, ns, keep, n_sink, n_recent,
                                    self._flat("d_score", d_score, torch.float32, n_layers, ns, nh, width), width,
-                                   self._flat("d_len", d_len, i32, ns), self._flat("d_page_table", d_page_table, i32, *d_page_table.shape),
-                                   d_page_table.shape[1], self._flat("d_new_page_table", d_new_page_table, i32, ns, d_new_page_table.shape[1]),
-                                   d_new_page_table.shape[1], self._flat("d_kept", d_kept, i32, n_layers, ns, nh, keep),
+                                   self._flat("d_len", d_len, i32, ns), self._flat("d_page_table", d_page_table, i32, ns, columns), columns,
+                                   self._flat("d_new_page_table", d_new_page_table, i32, ns, new_columns), new_columns,
+                                   self._flat("d_kept", d_kept, i32, n_layers, ns, nh, keep),
                                    self._flat("score_out", score_out, torch.float32, n_layers, ns, nh, width),
                                    self._flat("d_new_len", d_new_len, i32, ns), self._raw_stream()))
 
     def _cache_use(self, n_seq, position, score_in, score_out, decay):
-        shape = (self.cfg.n_layers, n_seq, self.cfg.n_heads, 0 if score_out is None else score_out.shape[3])
+        shape = (self.cfg.n_layers, n_seq, self.cfg.n_heads, 0 if score_out is None else self._sizes("score_out", score_out, 4)[3])
         return CacheUse(self._flat("position", position, torch.int32, n_seq), self._flat("score_in", score_in, torch.float32, *shape),
                         self._flat("score_out", score_out, torch.float32, *shape), shape[3], decay)
 

@@ -3,6 +3,7 @@ import ctypes
 import math
 
 import pytest
+import torch
 
 from paper_2510_08666_amd import binding as b
 
@@ -18,3 +19,40 @@ def test_rotary_rules_stay_in_float32s_range():
                dict(scaling="yarn", factor=2.0, original_positions=64, magnitude=1e39), dict(theta=math.nan), dict(theta=-1.0)):
         assert size(**kw) == 0, kw
         assert b.last_error() != ""
+
+
+class Host(b.Context):
+    """A context's checks of its arguments on host tensors; nothing of the library behind it."""
+
+    def __init__(self, heads, head_dim, layers=1):
+        self.cfg = type("Heads", (), dict(n_heads=heads, head_dim=head_dim, n_layers=layers))
+        self.h, self._dtype, self._index = None, torch.float32, -1      # (where host tensors are)
+
+    def _raw_stream(self):
+        return 0
+
+
+def test_missing_tensors_and_wrong_dimensions():
+    c = Host(2, 64)
+    rows, table = torch.zeros(3, 128), torch.zeros(1, 4, dtype=torch.int32)
+    with pytest.raises(b.DinferError):      # what fits reaches the library, which knows no such context
+        c.kv_append(0, [3], None, table, rows, rows, rows, rows)
+    append = dict(layer=0, lens=[3], d_past=None, d_page_table=table, d_q=rows, d_k=rows, d_v=rows, d_q_out=rows)
+    attend = dict(layer=0, lens=[3], d_past=None, d_page_table=table, d_q=rows, d_out=rows)
+    score = dict(layer=0, lens=[3], d_past=None, d_page_table=table, d_q=rows, d_score_out=torch.zeros(1, 2, 9))
+    evict = dict(first_layer=0, n_layers=1, keep=5, n_sink=0, n_recent=0, d_score=torch.zeros(1, 1, 2, 9), d_len=torch.zeros(1, dtype=torch.int32),
+                 d_page_table=table, d_new_page_table=table.clone(), d_kept=torch.zeros(1, 1, 2, 5, dtype=torch.int32),
+                 d_new_len=torch.zeros(1, dtype=torch.int32))
+    for fn, base, names in ((c.kv_append, append, ("d_page_table", "d_k", "d_v", "d_q_out")), (c.attend, attend, ("d_page_table", "d_q", "d_out")),
+                            (c.kv_score, score, ("d_page_table", "d_q", "d_score_out")),
+                            (c.kv_evict, evict, ("d_page_table", "d_new_page_table", "d_score"))):
+        with pytest.raises(b.DinferError):
+            fn(**base)
+        for n in names:
+            for bad in (None, base[n].reshape(-1)):
+                with pytest.raises(ValueError, match=n):
+                    fn(**{**base, n: bad})
+    with pytest.raises(ValueError, match="rotary_table"):
+        c.kv_append(**append, rotary=b.rotary(64), rotary_table=torch.zeros(64))
+    with pytest.raises(ValueError, match="score_out"):
+        c._cache_use(1, None, None, torch.zeros(9), 1.0)
