@@ -91,7 +91,8 @@ def rotary_table(rot, max_pos, device="cuda:0"):
     if n == 0:
         raise DinferError(-1, last_error())
     t = torch.empty((2, int(max_pos), rot.rotary_dim // 2), dtype=torch.float32, device=device)
-    _check(lib.dinfer_rotary_table(ctypes.byref(rot), int(max_pos), _ptr(t), n, _stream()))
+    with torch.cuda.device(t.device):      # (the kernel and its stream are the table's GPU's, whichever is current)
+        _check(lib.dinfer_rotary_table(ctypes.byref(rot), int(max_pos), _ptr(t), n, _stream()))
     return t
 
 

@@ -56,3 +56,39 @@ def test_missing_tensors_and_wrong_dimensions():
         c.kv_append(**append, rotary=b.rotary(64), rotary_table=torch.zeros(64))
     with pytest.raises(ValueError, match="score_out"):
         c._cache_use(1, None, None, torch.zeros(9), 1.0)
+
+
+def test_rotary_table_of_another_gpu(monkeypatch):
+    """The table is filled by the GPU that holds it, on that GPU's stream: the library is called with that one current."""
+    current, calls = ["cuda:0"], []
+
+    class Current:
+        def __init__(self, device):
+            self.device, self.old = str(device), None
+
+        def __enter__(self):
+            self.old, current[0] = current[0], self.device
+
+        def __exit__(self, *_):
+            current[0] = self.old
+
+    class Lib:
+        @staticmethod
+        def dinfer_rotary_table_bytes(rot, n):
+            return 64 * 4 * n
+
+        @staticmethod
+        def dinfer_rotary_table(rot, n, table, size, stream):
+            calls.append((current[0], stream))
+            return 0
+
+    class Table:
+        device = "cuda:1"
+
+    monkeypatch.setattr(b, "lib", Lib)
+    monkeypatch.setattr(b, "_stream", lambda: "stream of " + current[0])
+    monkeypatch.setattr(b, "_ptr", lambda t: 0)
+    monkeypatch.setattr(b.torch.cuda, "device", Current)
+    monkeypatch.setattr(b.torch, "empty", lambda *a, **kw: Table())
+    b.rotary_table(b.rotary(64), 100, "cuda:1")
+    assert calls == [("cuda:1", "stream of cuda:1")] and current == ["cuda:0"]
