@@ -359,7 +359,7 @@ int dinfer_kv_append(dinfer_ctx* ctx, int32_t layer, int32_t n_seq, const int32_
  *   d_visible  [T] or null (every token sees all new tokens): bit j set = the token sees its sequence's new token j.  A tree of
  *              drafts, a causal run, or padding that nobody sees; needs h_lens[s] <= 64.  What lies in keys and values a token does not
  *              see, infinities and NaN included, does not reach it.  A token that sees nothing gets zeros.
- *   scale      of the scores; 0: 1/sqrt(head_dim).
+ *   scale      of the scores, at most 1.7e38; 0: 1/sqrt(head_dim).
  *   d_out      [T] rows of n_q_heads heads.
  *   d_lse      [T][n_q_heads] float32, or null: logarithm of every row's sum of exponentials (-infinity: sees nothing).
  * One call takes fewer than 2^31 meetings of 32 rows with 32 positions, counted as if every cache were full (DINFER_EUNSUPPORTED):

@@ -1052,7 +1052,7 @@ static int check_rows(const dinfer_ctx* c, const char* name, const void* p, int6
   return DINFER_OK;
 }
 static int check_scale(const dinfer_ctx* c, float scale, float* out) {
-  if (!(scale >= 0.f && scale < INFINITY)) return fail(DINFER_EINVAL, "scale %g", (double)scale);
+  if (!(scale >= 0.f && scale <= FLT_MAX / 2)) return fail(DINFER_EINVAL, "scale %g", (double)scale);      // (times log2(e): finite)
   *out = scale > 0.f ? scale : 1.f / sqrtf((float)c->cfg.head_dim);
   return DINFER_OK;
 }

@@ -88,3 +88,23 @@ def test_ramped_frequencies(m, r, original, fast, slow, magnitude):
 def test_ramped_frequencies_that_do_not_stretch(m, factor):
     """A factor of at most one leaves cosines and sines their size."""
     check_table(m, 64, 300, "yarn", 10000.0, factor, 2048)
+
+
+def test_largest_scale(m):
+    """A scale whose product with log2(e) is no float32 number is refused; below it scores of zero stay zero."""
+    import torch
+    c = m.Cache("bf16", 2, 64, [3], [200], seed=91)
+    q = torch.zeros(3, 128, dtype=torch.bfloat16, device=m.DEV)
+    out, lse, score = torch.ones_like(q), torch.empty(3, 2, device=m.DEV), torch.zeros(1, 2, 203, device=m.DEV)
+    for scale in (3e38, 1.8e38):
+        with pytest.raises(m.binding.DinferError):
+            c.ctx.attend(0, [3], c.d_past, c.d_table, q, out, scale=scale, lse=lse)
+        with pytest.raises(m.binding.DinferError):
+            c.ctx.kv_score(0, [3], c.d_past, c.d_table, q, score, scale=scale)
+    torch.cuda.synchronize()
+    assert (out == 1).all() and (score == 0).all()
+    c.ctx.attend(0, [3], c.d_past, c.d_table, q, out, scale=1e38, lse=lse)
+    c.ctx.kv_score(0, [3], c.d_past, c.d_table, q, score, scale=1e38)
+    m.check_attention(c, q, 1, out, lse, scale=1e38)
+    assert (score - 3 / 203).abs().max() <= 3 / 203 * 2.0 ** -18
+    c.close()
