@@ -1257,8 +1257,9 @@ int dinfer_step_scored(dinfer_ctx* c, int32_t n_seq, int32_t block_len, int32_t*
                        const int32_t* d_prefix_len, const int32_t* d_page_table, int32_t pt_stride,
                        const dinfer_decode* decode, const dinfer_cache_use* use, float* d_conf, int32_t* d_argmax,
                        int32_t* d_n_committed, void* stream) {
+  if (!c) return fail(DINFER_EINVAL, "context is null");
   int rc = check_use(use);
-  if (rc != DINFER_OK) return rc;
+  if (rc != DINFER_OK || (rc = check_device(c)) != DINFER_OK) return rc;
   return step_impl(c, n_seq, block_len, d_block_tokens, d_mask, d_prefix_len, d_page_table, pt_stride, decode, d_conf,
                    d_argmax, d_n_committed, (hipStream_t)stream, nullptr, nullptr, nullptr, use);
 }
@@ -1268,7 +1269,7 @@ int dinfer_refresh_block_scored(dinfer_ctx* c, int32_t n_seq, int32_t block_len,
                                 const dinfer_cache_use* use, void* stream) {
   int rc = check_block_args(c, n_seq, block_len, d_block_tokens, d_prefix_len, d_page_table, pt_stride);
   if (rc != DINFER_OK) return rc;
-  if ((rc = check_use(use)) != DINFER_OK) return rc;
+  if ((rc = check_use(use)) != DINFER_OK || (rc = check_device(c)) != DINFER_OK) return rc;
   hipStream_t st = (hipStream_t)stream;
   rc = forward(c, uniform_span(n_seq, block_len), d_block_tokens, d_prefix_len, d_page_table, pt_stride, false, st, nullptr, use);
   if (rc != DINFER_OK) return rc;

@@ -108,3 +108,24 @@ def test_largest_scale(m):
     m.check_attention(c, q, 1, out, lse, scale=1e38)
     assert (score - 3 / 203).abs().max() <= 3 / 203 * 2.0 ** -18
     c.close()
+
+
+def test_another_current_gpu_is_refused(m):
+    """Every operator, the scored step and the scored refresh want the context's GPU to be the current one."""
+    import torch
+    if torch.cuda.device_count() < 2:
+        pytest.skip("needs two GPUs")
+    c = m.Cache("bf16", 4, 64, [9], [40], seed=92)
+    q, out, score = c.randn(9, 256), c.randn(9, 256), torch.zeros(1, 4, 60, device=m.DEV)
+    n, kept = torch.zeros(1, dtype=torch.int32, device=m.DEV), torch.zeros(1, 1, 4, 5, dtype=torch.int32, device=m.DEV)
+    tok, mask = torch.zeros(1, 32, dtype=torch.int32, device=m.DEV), torch.zeros(1, dtype=torch.int64, device=m.DEV)
+    conf = torch.zeros(1, 32, device=m.DEV)
+    with torch.cuda.device(1):
+        for call in (lambda: c.ctx.kv_append(0, [9], c.d_past, c.d_table, q, q, q, out), lambda: c.ctx.attend(0, [9], c.d_past, c.d_table, q, out),
+                     lambda: c.ctx.kv_score(0, [9], c.d_past, c.d_table, q, score),
+                     lambda: c.ctx.kv_evict(0, 1, 5, 0, 0, score[None], c.d_past, c.d_table, c.d_table.clone(), kept, n),
+                     lambda: c.ctx.step_scored(tok, mask, c.d_past, c.d_table, 0.5, 0, conf, tok.clone(), n),
+                     lambda: c.ctx.refresh_block_scored(tok, c.d_past, c.d_table)):
+            with pytest.raises(m.binding.DinferError, match="current device"):
+                call()
+    c.close()
