@@ -1,7 +1,13 @@
-"""The paged cache's operators in their larger forms, and in settings of the rotation that change its angles."""
+"""The paged cache's operators in their larger forms, the step's rotary positions and the refresh's scores, and settings of the rotation that
+change its angles."""
 import math
 
+import numpy as np
 import pytest
+
+import dinfer_inputs as di
+import test_gpu_cache_ops as ops
+from harness import GpuRun, make_case
 
 pytestmark = pytest.mark.gpu
 
@@ -129,3 +135,116 @@ def test_another_current_gpu_is_refused(m):
             with pytest.raises(m.binding.DinferError, match="current device"):
                 call()
     c.close()
+
+
+# ------------------------------------------------------------------------------------------------ larger forms
+
+@pytest.mark.parametrize("dtype,heads,hd", [("bf16", 35, 128), ("bf16", 35, 64), ("f32", 34, 128), ("f32", 33, 64)])
+@pytest.mark.parametrize("dim,interleaved,scaling,norm,custom", [(0, False, "plain", True, False), (2, True, "ntk", False, True),
+                                                                 (20, False, "yarn", True, True), (20, True, "linear", False, False)])
+def test_append_four_heads_per_workgroup(m, monkeypatch, dtype, heads, hd, dim, interleaved, scaling, norm, custom):
+    """64 ragged sequences fill the chip with workgroups of four heads (8192 meetings of pages and heads, the last workgroup's heads not all
+    there): norms, both layouts of pairs, rotations that end inside a lane's features and those that do not."""
+    lens, past = [7 * s % 41 for s in range(64)], [13 * s % 211 for s in range(64)]
+    assert sum((n + 14) // 16 + 1 if n else 0 for n in lens) * heads * 2 >= 8192
+    monkeypatch.setattr(ops, "APPENDS", [(lens, past)])
+    ops.test_append(m, dtype, heads, hd, 0, dim, interleaved, scaling, norm, 1, custom)
+
+
+@pytest.mark.parametrize("dtype,heads,hd", ops.SHAPES)
+@pytest.mark.parametrize("past,keep,sink,recent", [([4000, 1025, 3], 1024, 4, 64), ([2049, 1024, 2048], 2048, 0, 0), ([1500], 1, 0, 0),
+                                                   ([4094, 0, 1026], 777, 700, 77)])
+def test_evict_up_to_4096_positions(m, dtype, heads, hd, past, keep, sink, recent):
+    """Sixteen scores per thread of four waves."""
+    assert 1024 < max(past) + 2 <= 4096
+    ops.test_evict(m, dtype, heads, hd, past, keep, sink, recent)
+
+
+# ------------------------------------------------------------------------------------------------ the step
+
+def run_of(dtype, n_seq, block, lo, hi, seed, columns):
+    """The tiny model behind ragged prompts, page-table rows of `columns` pages."""
+    cfg = di.configs.scaled(di.model_preset("tiny"), dtype=dtype, n_layers=2, logit_scale=1.0)
+    cfg, w, inp = make_case(di.Workload("forms", cfg, n_seq, block, lo, hi, threshold=0.9, seed_index=seed))
+    table = np.random.default_rng(seed).permutation(n_seq * columns).astype(np.int32).reshape(n_seq, columns)
+    inp = di.configs.WorkloadInputs(inp.prefix_tokens, inp.block_tokens, inp.mask_bits, inp.prefix_len, table, n_seq * columns)
+    g = GpuRun(cfg, w, inp, max(n_seq * block, int(inp.prefix_len.sum())), columns * 16)
+    g.ctx.kv.zero_()
+    g.prefill()
+    return cfg, w, inp, g
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n_seq,block", [(1, 32), (2, 32), (3, 40), (5, 64), (16, 64)])
+def test_positions_of_ones_own(dtype, n_seq, block):
+    """The first layer's keys and values depend on tokens and rotary positions alone: those of a block behind p cached positions that is turned
+    as at P are, bit for bit, those of the same block behind P cached positions.  (By the number of tokens all forms of the projection.)"""
+    cfg, w, inp, g = run_of(dtype, n_seq, block, 20, 300, 170 + n_seq, 40)
+    torch = g.torch
+    tok0, mask0 = g.tokens.clone(), g.mask.clone()
+    p = g.prefix_len.clone()
+    at = (p + 40 * torch.arange(n_seq, device=g.dev, dtype=torch.int32) % 170 - 11).contiguous()
+
+    def rows(first):
+        return [torch.cat([g.ctx.kv_read(0, g.page_table[s], int(first[s]), block)[i] for s in range(n_seq)]).clone() for i in (0, 1)]
+
+    for fn in ("step", "refresh"):
+        g.tokens.copy_(tok0)
+        g.mask.copy_(mask0)
+        where = at.clone()
+        if fn == "step":
+            g.ctx.step_scored(g.tokens, g.mask, p, g.page_table, 0.9, 0, g.conf, g.argmax, g.n_committed, position=where)
+        else:
+            g.ctx.refresh_block_scored(g.tokens, p.clone(), g.page_table, position=where)
+        torch.cuda.synchronize()
+        assert torch.equal(where, at + (block if fn == "refresh" else 0))
+        got = rows(p)
+        g.tokens.copy_(tok0)
+        g.mask.copy_(mask0)
+        g.ctx.step(g.tokens, g.mask, at, g.page_table, 0.9, 0, g.conf, g.argmax, g.n_committed)
+        torch.cuda.synchronize()
+        want = rows(at)
+        assert got[0].any() and all(torch.equal(a, b) for a, b in zip(got, want)), fn
+    g.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n_seq,block,lo,hi,columns", [(1, 32, 100, 100, 40), (3, 13, 20, 900, 60), (2, 64, 1100, 1300, 96), (5, 64, 20, 200, 40)])
+def test_scores_of_a_refresh(dtype, n_seq, block, lo, hi, columns):
+    """A refresh leaves the scores of its block's queries: layer 0's from the definition, every layer's sum to one per query, and all are those that
+    a step on the same tokens leaves."""
+    cfg, w, inp, g = run_of(dtype, n_seq, block, lo, hi, 180 + n_seq, columns)
+    torch = g.torch
+    width = int(inp.prefix_len.max()) + block + 4
+    old = torch.rand((cfg.n_layers, n_seq, cfg.n_heads, width), device=g.dev)
+    scores, p = [torch.full_like(old, -1.0) for _ in range(2)], g.prefix_len.clone()
+    tok0 = g.tokens.clone()
+    g.ctx.refresh_block_scored(g.tokens, p, g.page_table, score_in=old, score_out=scores[0], decay=0.5)
+    assert torch.equal(p, g.prefix_len + block) and torch.equal(g.tokens, tok0)
+    g.ctx.step_scored(g.tokens, g.mask, g.prefix_len, g.page_table, 0.9, 0, g.conf, g.argmax, g.n_committed, score_in=old, score_out=scores[1],
+                      decay=0.5)
+    torch.cuda.synchronize()
+    assert torch.equal(scores[0], scores[1])
+    f64 = lambda a: (di.configs.bf16_to_f32(a) if a.dtype == np.uint16 else a).astype(np.float64)
+    emb, wq, hd, nh = f64(w["emb"]), f64(w["layers"][0]["wq"]), cfg.head_dim, cfg.n_heads
+    for s in range(n_seq):
+        q0, n = int(inp.prefix_len[s]), int(inp.prefix_len[s]) + block
+        gathered = (scores[0][:, s, :, :n].double() - 0.5 * old[:, s, :, :n].double()).cpu().numpy()
+        assert (scores[0][:, s, :, n:] == -1).all()
+        # weights: a few steps of 2^-24 each and of the old score; n of them
+        assert np.abs(gathered.sum(-1) - block).max() <= block * 2.0 ** -14 + n * 2.0 ** -24
+        x = emb[inp.block_tokens[s]]
+        x = x / np.sqrt((x * x).mean(-1, keepdims=True) + cfg.rms_eps) * w["layers"][0]["attn_gain"]
+        q = (x @ wq.T).reshape(block, nh, hd)
+        ang = (q0 + np.arange(block))[:, None] * cfg.rope_theta ** (-2.0 * np.arange(hd // 2) / hd)
+        cs, sn = np.cos(ang)[:, None], np.sin(ang)[:, None]
+        q = np.concatenate([q[..., :hd // 2] * cs - q[..., hd // 2:] * sn, q[..., hd // 2:] * cs + q[..., :hd // 2] * sn], -1)
+        k = g.read_kv(s, 0, 0, n)[0].astype(np.float64).reshape(-1, nh, hd)
+        for h in range(nh):
+            z = q[:, h] @ k[:, h].T / np.sqrt(hd)
+            e = np.exp(z - z.max(-1, keepdims=True))
+            ref = (e / e.sum(-1, keepdims=True)).sum(0)
+            # queries are kept to 2^-16 (two bfloat16 planes) or float32: a score moves by at most that of sum |q k| scale
+            bar = 2 * np.abs(q[:, h]).max() * np.abs(k[:, h]).max() * np.sqrt(hd) * 2.0 ** -14 + 2.0 ** -14
+            assert np.abs(gathered[0, h] - ref).max() <= bar * ref.max() + 2.0 ** -24, (s, h)
+    g.close()
