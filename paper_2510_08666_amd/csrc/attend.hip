@@ -138,10 +138,10 @@ __device__ inline float log_sum(float m, float l) { return l == 0.f ? -INFINITY 
 // parts of equal length, a workgroup takes one part, and attend_merge_kernel joins the parts of a pair.  The lengths are on
 // the device, so every wave works the plan out for itself, a lane per sequence.  A part has `per` key tiles at most: with few pairs as
 // many as leave about as many parts as workgroups run at a time, counting half a part per pair for the rounding (a few
-// workgroups more than fit run alone behind the others: 16 sequences of 17 to 32 tokens behind 256 to 2048, 608 of them 39.6 us, 496
-// 36.9); with many pairs the workgroups' share of all tiles, the longest parts first, so that the short ones fill the gaps; and at
-// least min_part (64 drafts behind 4096 keys: 8 tiles 22.9 us, 12 18.7).  A pair of up to min_cut tiles is left whole: its waves
-// have most of what they need under way at once, and joining costs more than they take.
+// workgroups more than fit run alone behind the others: 16 sequences of 17 to 32 tokens behind 256 to 2048, 608 of them 44.1 us with the
+// join, 496 42.3); with many pairs the workgroups' share of all tiles, the longest parts first, so that the short ones fill the gaps; and at
+// least min_part (64 drafts behind 4096 keys: 8 tiles 23.7 us, 12 19.5).  A pair of up to min_cut tiles is left whole: a wave
+// has six of them at most to walk, and joining (a launch of 3 to 5 us) costs more than they take.
 // In float32 a tile keeps a wave's matrix unit busy for 1.7 us: a pair is cut much earlier (3 sequences behind 64 to 901 keys 20.4 -> 12.3 us).
 template <typename E> constexpr int min_cut() { return sizeof(E) == 2 ? 24 : 8; }
 template <typename E> constexpr int min_part() { return sizeof(E) == 2 ? 12 : 4; }
@@ -485,12 +485,13 @@ __global__ __launch_bounds__(ATTEND_WAVES * WAVE, (attend_waves_per_simd<E, HD>(
 
 // Many rows (grouped query heads): a workgroup takes WAVES row tiles of a head, one per wave, and every key tile goes through LDS
 // once for all of them, two tiles a turn, double buffered, the turn after next on its way in registers; in the form above
-// each wave would fetch it for itself, and the compute unit's cache bounds the launch (48 sequences of 31 to 64 tokens with four
-// query heads per cache head behind 1000 to 8000: 467 us).  A wave keeps its queries and output in registers, nothing is folded.
-// Bound by the read of K and V, so a workgroup takes up to 256 rows (four waves and 128 rows, two workgroups per compute unit: 300 to
-// 370 us, 1.35 GB fetched; eight waves 263).  What a turn takes now, 2.4 us, is none of its bounds alone (counters: matrix units busy
-// 31 % of the time, LDS 22 %): waves wait for each other.  Without effect: two turns of loads under way, priorities or half a
-// turn's distance between the waves of a SIMD, output products between the second tile's exponentials, deeper rings.
+// each wave would fetch it for itself (48 sequences of 31 to 64 tokens with four query heads per cache head behind 1000 to 8000: 370 us
+// with the join).  A wave keeps its queries and output in registers, nothing is folded.  A workgroup takes up to 256 rows, so that K and
+// V are read fewer times (four waves and 128 rows, two workgroups per compute unit: 368 us; eight waves 332, 318 without the join).
+// What a turn takes now, 2.9 us, is none of its bounds alone (counters: matrix units busy 38 % of the time, vector units 36 %, LDS
+// 18 %): scores, exponentials and output are one chain in each wave, and waves wait for each other at every turn.  Without effect, with
+// one plane of weights: two turns of loads under way, priorities or half a turn's distance between the waves of a SIMD, output products
+// between the second tile's exponentials, deeper rings.  The second plane of weights took 60 us, split in front of its products 69.
 template <int HD> constexpr size_t attend_rows_lds() { return (size_t)2 * 4 * (HD / ET<bf16_t>::KS) * WAVE * 16 + ATTN_MAX_PAGES * 4; }
 template <int HD, int WAVES>
 __global__ __launch_bounds__(WAVES * WAVE, 2) void attend_rows_kernel(AttendArgs a, const int32_t* __restrict__ live) {
@@ -819,7 +820,7 @@ static int64_t most_meetings(const AttendArgs& a) {
   return row_tiles * a.geom.n_heads * ((a.tok.limit + TILE - 1) / TILE);
 }
 // Two row tiles per workgroup where a sequence has more than one; more than two: the form whose tiles go through LDS, where there is
-// work enough for it.  Its workgroups are few and take 3 us a turn, however little there is: of 8 cache heads of 4 queries each, 60
+// work enough for it.  Its workgroups are few and take 2.9 us a turn, however little there is: of 8 cache heads of 4 queries each, 60
 // tokens behind 3000 positions take 38.8 us in it and 20.3 in two row tiles, eight sequences of them (49 thousand meetings) 65 and 63,
 // sixteen 98 and 92, 24 (148 thousand) 178 and 153, 32 163 and 202, 48 278 and 298.  How a call's parts fill its 256 places moves the
 // crossover: 16 heads of 8 queries and 20 tokens 151 and 133 at 91 thousand, 138 and 154 at 121, 4 heads of 8 and 64 tokens 91 and 95 at 97,
@@ -864,7 +865,7 @@ bool configure_attend() {
 // no atomics, the same bits every time.  A wave holds KT key tiles in registers, all their loads under way at once, and meets them with
 // one row tile after the other.  Bound by the read of K; with many rows by the matrix instructions and the queries' second
 // reads, which KT tiles share (16 KB of keys per wave: what fits the registers beside the queries).  16 sequences of 17 to 32 tokens
-// behind 256 to 4096 positions, 150 MB: 34.4 us, 4.3 TB/s with the start of every workgroup (lengths, pages, keys: three dependent loads).
+// behind 256 to 4096 positions, 150 MB: 35.7 us, 4.2 TB/s with the start of every workgroup (lengths, pages, keys: three dependent loads).
 // ------------------------------------------------------------------------------------------------
 constexpr int SCORE_WAVES = 4;
 // A key's weight over the 16 rows in a lane's registers.  lse: of the tile's rows, times log2(e), infinity for those that weigh nothing;

@@ -181,8 +181,8 @@ template <typename E, int HD, int HB> static void launch_append_hb(const AppendA
   else append_kernel<E, HD, HB, false><<<grid, APPEND_THREADS, 0, st>>>(a, groups);
 }
 // Four heads per workgroup once that leaves the chip full of workgroups, else as few as a pass takes (16 heads of 128: a block of 32
-// tokens 4.3 us against 6.5 with four heads, 16 sequences of 1 to 64 tokens 6.9 against 9.4; four prompts of 333 to 1811 tokens, 108 MB,
-// 26 with four heads, 4.1 TB/s, a microsecond more with one).
+// tokens 4.4 us against 6.5 with four heads, 16 sequences of 1 to 64 tokens 6.9 against 9.4; four prompts of 333 to 1811 tokens, 108 MB,
+// 27 with four heads, 4.0 TB/s, a microsecond more with one).
 constexpr int APPEND_FULL = 2048;
 template <typename E, int HD> static void launch_append_t(const AppendArgs& a, const SeqSpan& groups, hipStream_t st) {
   constexpr int LEAST = sizeof(E) * HD == 128 ? 2 : 1;
@@ -214,7 +214,7 @@ void launch_append(bool bf16, const AppendArgs& a, hipStream_t st) {
 // digit where its sums from above reach what is still wanted; the search ends where a digit is taken whole.  The counts are
 // whole numbers, so the order of the atomics does not matter.  Positions keep their order: a position's place is the number of
 // chosen ones in front of it, from ballots and one prefix sum over the waves' counts.  Bound by the latency of these
-// turns (512 heads of up to 4096 scores 15.2 us; a search two bits at a time by ballots took 16 turns, 29 us).
+// turns (512 heads of up to 4096 scores 15.1 us; a search two bits at a time by ballots took 16 turns, 35 us).
 __device__ inline uint32_t score_order(float v) {
   const uint32_t b = __float_as_uint(v + 0.f);                           // (-0 + 0 is 0)
   const uint32_t o = b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
