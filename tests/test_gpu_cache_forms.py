@@ -248,3 +248,56 @@ def test_scores_of_a_refresh(dtype, n_seq, block, lo, hi, columns):
             bar = 2 * np.abs(q[:, h]).max() * np.abs(k[:, h]).max() * np.sqrt(hd) * 2.0 ** -14 + 2.0 ** -14
             assert np.abs(gathered[0, h] - ref).max() <= bar * ref.max() + 2.0 ** -24, (s, h)
     g.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n_seq,block,lo,hi,columns", [(2, 1, 1, 3, 4), (2, 32, 100, 900, 70), (3, 64, 20, 60, 12)])
+def test_scored_step_and_refresh_captured(dtype, n_seq, block, lo, hi, columns):
+    """A step with scores and a refresh with scores in one graph: every replay leaves what the eager calls left, with eager work on other tokens between
+    the replays.  The score rows end in the block of the longest sequence."""
+    cfg, w, inp, g = run_of(dtype, n_seq, block, lo, hi, 190 + n_seq, columns)
+    torch = g.torch
+    width = int(inp.prefix_len.max()) + block // 2
+    state = dict(tokens=g.tokens, mask=g.mask, conf=g.conf, argmax=g.argmax, n=g.n_committed, length=g.prefix_len.clone(),
+                 at=(g.prefix_len + 2).contiguous(), step=torch.zeros((cfg.n_layers, n_seq, cfg.n_heads, width), device=g.dev),
+                 refresh=torch.zeros((cfg.n_layers, n_seq, cfg.n_heads, width), device=g.dev))
+    start = {k: v.clone() for k, v in state.items()}
+    kv0 = g.ctx.kv.clone()
+
+    def run():
+        g.ctx.step_scored(g.tokens, g.mask, state["length"], g.page_table, 0.02, 0, g.conf, g.argmax, g.n_committed, position=state["at"],
+                          score_out=state["step"])
+        g.ctx.refresh_block_scored(g.tokens, state["length"], g.page_table, position=state["at"], score_in=state["step"], score_out=state["refresh"],
+                                   decay=0.9)
+
+    def reset():
+        for k, v in start.items():
+            state[k].copy_(v)
+        g.ctx.kv.copy_(kv0)
+
+    run()
+    torch.cuda.synchronize()
+    want = {k: v.clone() for k, v in state.items()}
+    kv = g.ctx.kv.clone()
+    assert want["refresh"].any() and torch.equal(want["at"], start["at"] + block)
+    reset()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for rep in range(4):
+        reset()
+        g.tokens.copy_((start["tokens"] + 7 * rep + 1) % (cfg.vocab - 1))
+        run()
+        torch.cuda.synchronize()
+        reset()
+        graph.replay()
+        torch.cuda.synchronize()
+        for k, v in want.items():
+            assert torch.equal(state[k], v), (rep, k)
+        assert torch.equal(g.ctx.kv, kv), rep
+    g.close()
