@@ -415,6 +415,94 @@ int dinfer_refresh_block_scored(dinfer_ctx* ctx, int32_t n_seq, int32_t block_le
                                 int32_t* d_prefix_len, const int32_t* d_page_table, int32_t pt_stride,
                                 const dinfer_cache_use* use, void* stream);
 
+/* ---- Search over several continuations ----------------------------------------------------------------------------
+ * For programs that keep several hypotheses of a sequence: a prompt is read under dinfer_attend_ruled, dinfer_kv_fork makes
+ * its hypotheses, which share the pages that none of them writes, dinfer_beam_select chooses among their candidates,
+ * dinfer_kv_fork goes on with the chosen ones, and dinfer_kv_compact packs a pool whose pages have been scattered. */
+
+/* What a token of dinfer_attend_ruled sees.  The token at cache position p (d_past[s] + its place in the sequence) sees position j of
+ * its sequence's d_past[s] + h_lens[s] if and only if
+ *     d_first[t] <= j < d_end[t]   and   ( j < d_prefix[s]   or   ( j < e(p)  and  |p - j| < window ) )
+ *   block     0: e(p) has no bound (both directions).  b > 0: order in time by blocks of b positions behind the prefix, e(p) = the end of p's
+ *             block: d_prefix[s] for p inside the prefix, else d_prefix[s] + ((p - d_prefix[s]) / b + 1) * b.  1: causal.
+ *   window    0: no bound.
+ *   d_prefix  [n_seq] or null (0): positions that all tokens of the sequence see, one another included.
+ *   d_first, d_end [T] or null (0 | all): the token's document, as cache positions.
+ *   cap       0, or > 0: scores z become cap * tanh(z / cap).  At least 1e-30.
+ *   d_slope   [n_q_heads] float32 or null: slope * |p - j| is taken off the head's scores (behind the cap). */
+typedef struct {
+  int32_t block, window;
+  const int32_t *d_prefix, *d_first, *d_end;
+  float cap;
+  const float* d_slope;
+} dinfer_attend_rule;
+
+/* dinfer_attend with a rule in the place of visibility words, and any number of new tokens.  What lies in keys and values that a token
+ * does not see, infinities and NaN included, does not reach it; a token that sees nothing gets zeros (d_lse -infinity).  The bound
+ * on the size of a call is dinfer_attend's. */
+int dinfer_attend_ruled(dinfer_ctx* ctx, int32_t layer, int32_t n_seq, const int32_t* h_lens, const int32_t* d_past,
+                        const int32_t* d_page_table, int32_t pt_stride, const void* d_q, int64_t q_stride, int32_t n_q_heads,
+                        const dinfer_attend_rule* rule, float scale, void* d_out, int64_t out_stride, float* d_lse, void* stream);
+
+/* The n_keep best candidates of every sequence's n_rows rows of logits.  A row is a hypothesis, or an undecided position of one; token v
+ * of row r scores  d_score[r] + z[r][v] - log(sum over u of exp(z[r][u])).  Needs no context; works on the current GPU.
+ *   d_logits  n_seq * n_rows rows of `vocab` elements of `dtype` (DINFER_F32, DINFER_BF16), row_stride elements apart.  -infinity and NaN:
+ *             no candidate, no weight.  If there are +infinities in a row, they share its weight.
+ *   d_score   [n_seq][n_rows] float32; -infinity (or NaN): the row takes no part and is not read.
+ *   d_hold    [n_seq][n_rows] or null: >= 0: the hypothesis is finished, its only candidate is this token, at d_score[r].
+ *   d_row, d_token [n_seq][n_keep] out: the candidates, best first; equal scores: the lower row, then the lower token.  Where there are
+ *             fewer: -1 (d_score_out -infinity).
+ *   d_score_out [n_seq][n_keep] out; may not be d_score.
+ *   d_scratch 256-byte aligned, dinfer_beam_scratch_bytes (0: a size out of range), contents irrelevant.
+ * Scores are compared in 64 bits and rounded once.  n_keep <= 64, n_rows <= 1024, n_seq * n_rows <= 65535, vocab <= 2^24. */
+size_t dinfer_beam_scratch_bytes(int32_t n_seq, int32_t n_rows, int32_t vocab, int32_t n_keep);
+int dinfer_beam_select(const void* d_logits, int32_t dtype, int64_t row_stride, int32_t n_seq, int32_t n_rows, int32_t vocab,
+                       const float* d_score, const int32_t* d_hold, int32_t n_keep, int32_t* d_row, int32_t* d_token,
+                       float* d_score_out, void* d_scratch, size_t scratch_bytes, void* stream);
+
+/* Pages that several sequences may hold are counted by the caller's program in d_refs [n_pages]: how many page-table rows hold each page,
+ * 0 where it is free.  dinfer_kv_fork and dinfer_kv_compact read such counts and leave new ones in another buffer.  (A pool that starts
+ * empty has all counts 0; n_old = 0 hands out its first pages.)
+ *
+ * Makes the next n_new sequences out of the n_old present ones (0 <= n_old <= max_seqs, 1 <= n_new <= max_seqs), in all layers:
+ *   d_parent  [n_new]: sequence i continues old sequence d_parent[i] (-1, or no old sequence: it begins empty).  Old sequences
+ *             without children end.
+ *   d_len, d_held [n_old]: their cached positions, and how many columns of their page-table rows they hold (at least what the positions
+ *             take).
+ *   room      positions behind the cached ones that a new sequence gets pages for; rewrite: cached positions at its end that will
+ *             be written again (0: none; a refreshed block's length, a vicinity's look_back).
+ * With own = (len - rewrite, at least 0) / 16: columns in front of `own` are the parent's pages, shared.  Columns from `own` up to
+ * ceil((len + room) / 16) (at most new_pt_stride) are the sequence's own: the first child (lowest i) of a parent takes over the
+ * parent's page where nobody else holds it; all others are pages that were free before the call, the lowest first in the order of i and
+ * column, and what they hold of cached positions is copied, whole pages.
+ *   d_new_len, d_new_held [n_new], d_new_page_table [n_new][new_pt_stride] (-1 behind the held columns), d_new_refs [n_pages] out.  Pages
+ *             that the call frees can be handed out by the next one.
+ *   d_short   [1] out: 0, or how many free pages are missing: then nothing else is written.
+ *   h_states  (host) n_states <= 8 arrays of a row per sequence: d_out row i = d_in row d_parent[i] (zeros for a sequence that begins
+ *             empty).  row_bytes and addresses multiples of 4.
+ * No output may be an input.  n_pages <= 786432. */
+typedef struct {
+  const void* d_in;
+  void* d_out;
+  int64_t row_bytes;
+} dinfer_state;
+int dinfer_kv_fork(dinfer_ctx* ctx, int32_t n_old, int32_t n_new, const int32_t* d_parent, const int32_t* d_len, const int32_t* d_held,
+                   const int32_t* d_page_table, int32_t pt_stride, int32_t room, int32_t rewrite, const int32_t* d_refs,
+                   int32_t* d_new_len, int32_t* d_new_held, int32_t* d_new_page_table, int32_t new_pt_stride, int32_t* d_new_refs,
+                   int32_t* d_short, const dinfer_state* h_states, int32_t n_states, void* stream);
+
+/* Moves the pages in use (d_refs > 0) to the front of the pool, in all layers: with U of them, the k-th one from page U on goes
+ * to the k-th free page in front of U.  All page-table rows that hold pages have to follow.
+ *   d_held [n_seq], d_page_table [n_seq][pt_stride]: rows that are brought along, d_new_page_table out (-1 behind the held columns).
+ *   d_new_refs [n_pages] out.
+ *   d_moved   [2][n_pages] out: every page's new number (-1: it was free), for rows that the call is not given; then the pages that
+ *             moved, ascending, -1 behind them.
+ *   d_count   [2] out: U, and how many pages moved.
+ * No output may be an input.  1 <= n_seq <= max_seqs, n_pages <= 786432. */
+int dinfer_kv_compact(dinfer_ctx* ctx, int32_t n_seq, const int32_t* d_held, const int32_t* d_page_table, int32_t pt_stride,
+                      const int32_t* d_refs, int32_t* d_new_page_table, int32_t* d_new_refs, int32_t* d_moved, int32_t* d_count,
+                      void* stream);
+
 /* Test hooks.  dinfer_debug_logits recomputes the logits of the last forward's rows (n_rows must equal their
  * number) through the LM-head kernel's arithmetic and stores them: d_out [n_rows][vocab] float32.  dinfer_debug_get copies
  * an intermediate of the last forward: what = 0 residual stream leaving the last layer [T][hidden] f32;

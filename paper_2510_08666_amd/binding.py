@@ -29,7 +29,8 @@ EXPORTS = ["dinfer_weights_bytes", "dinfer_kv_bytes", "dinfer_workspace_bytes", 
            "dinfer_profile_every", "dinfer_profile_start", "dinfer_profile_stop", "dinfer_stream_read", "dinfer_debug_trace",
            "dinfer_debug_single_slice", "dinfer_generate_block_smooth", "dinfer_rotary_table_bytes", "dinfer_rotary_table",
            "dinfer_kv_append", "dinfer_attend", "dinfer_kv_score", "dinfer_kv_evict", "dinfer_step_scored",
-           "dinfer_refresh_block_scored"]
+           "dinfer_refresh_block_scored", "dinfer_attend_ruled", "dinfer_beam_scratch_bytes", "dinfer_beam_select",
+           "dinfer_kv_fork", "dinfer_kv_compact"]
 (STAGE_QKV, STAGE_ATTENTION, STAGE_OPROJ, STAGE_EXPERT_GATE_UP, STAGE_EXPERT_DOWN, STAGE_LM_HEAD,
  STAGE_ROUTER) = range(7)
 
@@ -75,6 +76,15 @@ class CacheUse(ctypes.Structure):
     _fields_ = [("d_position", c_vp), ("d_score_in", c_vp), ("d_score_out", c_vp), ("score_stride", c_i32), ("decay", c_f32)]
 
 
+class AttendRule(ctypes.Structure):
+    _fields_ = [("block", c_i32), ("window", c_i32), ("d_prefix", c_vp), ("d_first", c_vp), ("d_end", c_vp), ("cap", c_f32),
+                ("d_slope", c_vp)]
+
+
+class State(ctypes.Structure):
+    _fields_ = [("d_in", c_vp), ("d_out", c_vp), ("row_bytes", c_i64)]
+
+
 ROTARY_SCALINGS = {"plain": 0, "linear": 1, "ntk": 2, "yarn": 3}
 
 
@@ -104,6 +114,42 @@ def commit(d_conf, d_argmax, d_block_tokens, d_mask, decode, d_n_committed):
     n_seq, block_len = d_block_tokens.shape
     _check(lib.dinfer_commit(_ptr(d_conf), _ptr(d_argmax), n_seq, block_len, _ptr(d_block_tokens), _ptr(d_mask),
                              ctypes.byref(decode), _ptr(d_n_committed), _stream()))
+
+
+def beam_scratch(n_seq, n_rows, vocab, n_keep, device="cuda:0"):
+    """Device scratch buffer of beam_select."""
+    n = lib.dinfer_beam_scratch_bytes(int(n_seq), int(n_rows), int(vocab), int(n_keep))
+    if n == 0:
+        raise DinferError(-1, last_error())
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def beam_select(logits, score, row, token, score_out, scratch, hold=None):
+    """The best candidates (row, token) of every sequence (see dinfer_beam_select): logits [n_seq][n_rows][vocab] (float32 or bfloat16, a
+    sequence's rows as far apart as the others), score [n_seq][n_rows]; row, token, score_out [n_seq][n_keep] receive them."""
+    if logits is None or logits.dim() != 3 or logits.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("logits must be a float32 or bfloat16 tensor of 3 dimensions")
+    (ns, rows, vocab), (outer, stride, one) = logits.shape, logits.stride()
+    index = logits.get_device()
+    if index < 0 or one != 1 and vocab > 1 or ns > 1 and rows > 1 and outer != rows * stride:
+        raise ValueError("logits must be rows of contiguous elements, equally far apart, on a GPU")
+    if rows == 1:
+        stride = outer if ns > 1 else max(vocab, 1)
+    if row is None or row.dim() != 2:
+        raise ValueError("row must be a tensor of 2 dimensions")
+    keep = row.shape[1]
+    for name, t, dtype, shape in (("score", score, torch.float32, (ns, rows)), ("row", row, torch.int32, (ns, keep)),
+                                  ("token", token, torch.int32, (ns, keep)), ("score_out", score_out, torch.float32, (ns, keep)),
+                                  ("hold", hold, torch.int32, (ns, rows))):
+        if t is None and name == "hold":
+            continue
+        if t is None or t.dtype is not dtype or t.shape != shape or t.get_device() != index or not t.is_contiguous():
+            raise ValueError("%s must be a contiguous %s tensor %s on the logits' device" % (name, dtype, list(shape)))
+    if scratch is None or scratch.dtype is not torch.uint8 or scratch.get_device() != index or not scratch.is_contiguous():
+        raise ValueError("scratch must be a contiguous uint8 tensor on the logits' device")
+    with torch.cuda.device(index):
+        _check(lib.dinfer_beam_select(_ptr(logits), BF16 if logits.dtype is torch.bfloat16 else F32, stride, ns, rows, vocab, _ptr(score),
+                                      _ptr(hold), keep, _ptr(row), _ptr(token), _ptr(score_out), _ptr(scratch), scratch.numel(), _stream()))
 
 
 class DinferError(RuntimeError):
@@ -180,6 +226,18 @@ def _load():
                                      c_vp, c_vp]
     L.dinfer_refresh_block_scored.restype = c_i32
     L.dinfer_refresh_block_scored.argtypes = [c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, c_i32, P(CacheUse), c_vp]
+    L.dinfer_attend_ruled.restype = c_i32
+    L.dinfer_attend_ruled.argtypes = [c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, c_i32, c_vp, c_i64, c_i32, P(AttendRule), c_f32, c_vp,
+                                      c_i64, c_vp, c_vp]
+    L.dinfer_beam_scratch_bytes.restype = c_sz
+    L.dinfer_beam_scratch_bytes.argtypes = [c_i32, c_i32, c_i32, c_i32]
+    L.dinfer_beam_select.restype = c_i32
+    L.dinfer_beam_select.argtypes = [c_vp, c_i32, c_i64, c_i32, c_i32, c_i32, c_vp, c_vp, c_i32, c_vp, c_vp, c_vp, c_vp, c_sz, c_vp]
+    L.dinfer_kv_fork.restype = c_i32
+    L.dinfer_kv_fork.argtypes = [c_vp, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp, c_i32, c_i32, c_i32, c_vp, c_vp, c_vp, c_vp, c_i32, c_vp,
+                                 c_vp, P(State), c_i32, c_vp]
+    L.dinfer_kv_compact.restype = c_i32
+    L.dinfer_kv_compact.argtypes = [c_vp, c_i32, c_vp, c_vp, c_i32, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp]
     L.dinfer_commit.restype = c_i32
     L.dinfer_commit.argtypes = [c_vp, c_vp, c_i32, c_i32, c_vp, c_vp, P(Decode), c_vp, c_vp]
     L.dinfer_generate.restype = c_i32
@@ -510,6 +568,50 @@ class Context:
                                    self._flat("d_kept", d_kept, i32, n_layers, ns, nh, keep),
                                    self._flat("score_out", score_out, torch.float32, n_layers, ns, nh, width),
                                    self._flat("d_new_len", d_new_len, i32, ns), self._raw_stream()))
+
+    def attend_ruled(self, layer, lens, d_past, d_page_table, d_q, d_out, block=0, window=0, prefix=None, first=None, end=None, cap=0.0,
+                     slope=None, scale=0.0, lse=None):
+        """Attention of any number of new tokens over the cache under a rule (see dinfer_attend_rule): causal by blocks, window, prefix
+        [n_seq], documents first, end [T], capped scores, slopes [query heads]."""
+        tok, T = self._tokens(lens, d_past, d_page_table)
+        nq, i32 = self._sizes("d_q", d_q, 2)[1] // self.cfg.head_dim, torch.int32
+        rule = AttendRule(block, window, self._flat("prefix", prefix, i32, len(lens)), self._flat("first", first, i32, T),
+                          self._flat("end", end, i32, T), cap, self._flat("slope", slope, torch.float32, nq))
+        _check(lib.dinfer_attend_ruled(self.h, layer, *tok, *self._rows("d_q", d_q, T, nq), nq, rule, scale, *self._rows("d_out", d_out, T, nq),
+                                       self._flat("lse", lse, torch.float32, T, nq), self._raw_stream()))
+
+    def kv_fork(self, parent, d_len, d_held, d_page_table, refs, d_new_len, d_new_held, d_new_page_table, new_refs, short, room=0, rewrite=0,
+                states=()):
+        """The next sequences out of the present ones (see dinfer_kv_fork): parent [n_new]; d_len, d_held [n_old] and d_page_table
+        [n_old][columns] (all None: no old ones); refs, new_refs [n_pages]; short [1]; states: pairs of tensors, a row per old and per
+        new sequence."""
+        i32 = torch.int32
+        n_new, new_columns = self._sizes("d_new_page_table", d_new_page_table, 2)
+        n_old, columns = (0, 0) if d_page_table is None else self._sizes("d_page_table", d_page_table, 2)
+        rows = (State * max(len(states), 1))()
+        for k, (a, b) in enumerate(states):
+            for name, t, n in (("state %d" % k, a, n_old), ("new state %d" % k, b, n_new)):
+                if t.get_device() != self._index or not t.is_contiguous() or t.dim() < 1 or t.shape[0] < n:
+                    raise ValueError("%s must be a contiguous tensor of %d rows on the context's device" % (name, n))
+            if a.dtype is not b.dtype or a.shape[1:] != b.shape[1:]:
+                raise ValueError("state %d: rows of one type and size" % k)
+            rows[k] = State(a.data_ptr(), b.data_ptr(), b[:1].numel() * b.element_size())
+        _check(lib.dinfer_kv_fork(self.h, n_old, n_new, self._flat("parent", parent, i32, n_new), self._flat("d_len", d_len, i32, n_old),
+                                  self._flat("d_held", d_held, i32, n_old), self._flat("d_page_table", d_page_table, i32, n_old, columns), columns,
+                                  room, rewrite, self._flat("refs", refs, i32, self.n_pages), self._flat("d_new_len", d_new_len, i32, n_new),
+                                  self._flat("d_new_held", d_new_held, i32, n_new),
+                                  self._flat("d_new_page_table", d_new_page_table, i32, n_new, new_columns), new_columns,
+                                  self._flat("new_refs", new_refs, i32, self.n_pages), self._flat("short", short, i32, 1), rows, len(states),
+                                  self._raw_stream()))
+
+    def kv_compact(self, d_held, d_page_table, refs, d_new_page_table, new_refs, moved, count):
+        """Moves the pages in use to the front of the pool (see dinfer_kv_compact): moved [2][n_pages], count [2]."""
+        i32, (ns, columns) = torch.int32, self._sizes("d_page_table", d_page_table, 2)
+        _check(lib.dinfer_kv_compact(self.h, ns, self._flat("d_held", d_held, i32, ns), self._flat("d_page_table", d_page_table, i32, ns, columns),
+                                     columns, self._flat("refs", refs, i32, self.n_pages),
+                                     self._flat("d_new_page_table", d_new_page_table, i32, ns, columns),
+                                     self._flat("new_refs", new_refs, i32, self.n_pages), self._flat("moved", moved, i32, 2, self.n_pages),
+                                     self._flat("count", count, i32, 2), self._raw_stream()))
 
     def _cache_use(self, n_seq, position, score_in, score_out, decay):
         shape = (self.cfg.n_layers, n_seq, self.cfg.n_heads, 0 if score_out is None else self._sizes("score_out", score_out, 4)[3])

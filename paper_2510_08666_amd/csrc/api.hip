@@ -13,6 +13,7 @@
 #include "cache.hpp"
 #include "gemm.hpp"
 #include "kernels.hpp"
+#include "search.hpp"
 
 using namespace dinfer;
 
@@ -519,7 +520,7 @@ int dinfer_create(const dinfer_config* cfg, void* d_weights, size_t weights_byte
     delete c;
     return fail(DINFER_EHIP, "hipHostMalloc failed");
   }
-  if (!configure_kernels() || !configure_attention() || !configure_wide() || !configure_attend()) {
+  if (!configure_kernels() || !configure_attention() || !configure_wide() || !configure_attend() || !configure_ruled() || !configure_search()) {
     (void)hipHostFree(c->h_mask_pinned);
     delete c;
     return fail(DINFER_EHIP, "the runtime refused the kernels' LDS sizes");
@@ -1241,6 +1242,137 @@ int dinfer_kv_evict(dinfer_ctx* c, int32_t first_layer, int32_t n_layers, int32_
               n_recent, row < c->cfg.max_pos ? (int32_t)row : c->cfg.max_pos, d_score, score_stride, d_len, d_page_table,
               pt_stride, d_new_page_table, new_pt_stride, d_kept, d_score_out, d_new_len};
   launch_evict(c->bf16, a, (hipStream_t)stream);
+  HIP_TRY(hipGetLastError());
+  return DINFER_OK;
+}
+
+// ---- search over several continuations
+
+int dinfer_attend_ruled(dinfer_ctx* c, int32_t layer, int32_t n_seq, const int32_t* h_lens, const int32_t* d_past,
+                        const int32_t* d_page_table, int32_t pt_stride, const void* d_q, int64_t q_stride, int32_t n_q_heads,
+                        const dinfer_attend_rule* rule, float scale, void* d_out, int64_t out_stride, float* d_lse, void* stream) {
+  AttendArgs a{};
+  int rc = cache_tokens(c, layer, n_seq, h_lens, d_past, d_page_table, pt_stride, n_q_heads, &a.tok);
+  if (rc != DINFER_OK) return rc;
+  if (!rule) return fail(DINFER_EINVAL, "rule is null");
+  if (rule->block < 0 || rule->window < 0) return fail(DINFER_EINVAL, "block %d, window %d", rule->block, rule->window);
+  if (!(rule->cap == 0.f || (rule->cap >= 1e-30f && rule->cap <= FLT_MAX / 4))) return fail(DINFER_EINVAL, "cap %g", (double)rule->cap);
+  if ((rc = check_rows(c, "d_q", d_q, q_stride, n_q_heads)) != DINFER_OK) return rc;
+  if ((rc = check_rows(c, "d_out", d_out, out_stride, n_q_heads)) != DINFER_OK) return rc;
+  if ((rc = check_meetings(c, a.tok, n_q_heads)) != DINFER_OK) return rc;
+  if ((rc = check_scale(c, scale, &a.scale)) != DINFER_OK) return rc;
+  if ((rc = check_device(c)) != DINFER_OK) return rc;
+  a.group = n_q_heads / c->cfg.n_heads;
+  a.kv_layer = c->kv + (size_t)layer * c->kv_layer_bytes;
+  a.geom = c->geom;
+  a.q = d_q, a.q_stride = q_stride;
+  a.out = d_out, a.out_stride = out_stride;
+  a.lse = d_lse;
+  a.part = at<float>(c->ws, c->wsm.attend_part);
+  // (no cache is longer than ATTN_MAX_PAGES pages: longer blocks and windows are the same as these)
+  const int most = 2 * ATTN_MAX_PAGES * PAGE;
+  a.rule = AttendRule{rule->block < most ? rule->block : most, rule->window < most ? rule->window : most, rule->d_prefix, rule->d_first,
+                      rule->d_end, rule->cap, rule->d_slope};
+  if (a.tok.span.off[n_seq] == 0) return DINFER_OK;
+  launch_ruled(c->bf16, a, (hipStream_t)stream);
+  HIP_TRY(hipGetLastError());
+  return DINFER_OK;
+}
+
+static int check_select(int32_t n_seq, int32_t n_rows, int32_t vocab, int32_t n_keep) {
+  if (n_seq < 1 || n_rows < 1 || n_rows > MAX_SELECT_ROWS || (int64_t)n_seq * n_rows > 65535)
+    return fail(DINFER_EINVAL, "%d sequences of %d rows", n_seq, n_rows);
+  if (vocab < 1 || vocab > 1 << 24) return fail(DINFER_EINVAL, "vocab %d", vocab);
+  if (n_keep < 1 || n_keep > MAX_KEEP) return fail(DINFER_EINVAL, "n_keep %d outside [1, %d]", n_keep, MAX_KEEP);
+  return DINFER_OK;
+}
+size_t dinfer_beam_scratch_bytes(int32_t n_seq, int32_t n_rows, int32_t vocab, int32_t n_keep) {
+  if (check_select(n_seq, n_rows, vocab, n_keep) != DINFER_OK) return 0;
+  return select_scratch_bytes((int64_t)n_seq * n_rows, vocab, n_keep);
+}
+int dinfer_beam_select(const void* d_logits, int32_t dtype, int64_t row_stride, int32_t n_seq, int32_t n_rows, int32_t vocab,
+                       const float* d_score, const int32_t* d_hold, int32_t n_keep, int32_t* d_row, int32_t* d_token,
+                       float* d_score_out, void* d_scratch, size_t scratch_bytes, void* stream) {
+  if (!d_logits || !d_score || !d_row || !d_token || !d_score_out || !d_scratch) return fail(DINFER_EINVAL, "null pointer");
+  if (dtype != DINFER_F32 && dtype != DINFER_BF16) return fail(DINFER_EINVAL, "dtype %d", dtype);
+  const int rc = check_select(n_seq, n_rows, vocab, n_keep);
+  if (rc != DINFER_OK) return rc;
+  if (row_stride < vocab || (uintptr_t)d_logits % (dtype == DINFER_BF16 ? 2 : 4)) return fail(DINFER_EINVAL, "rows %lld elements apart", (long long)row_stride);
+  if (d_score_out == d_score || d_row == d_token) return fail(DINFER_EINVAL, "an output is another argument");
+  if ((uintptr_t)d_scratch & 255) return fail(DINFER_EINVAL, "d_scratch must be 256-byte aligned");
+  const size_t need = select_scratch_bytes((int64_t)n_seq * n_rows, vocab, n_keep);
+  if (scratch_bytes < need) return fail(DINFER_ENOSPACE, "scratch %zu < %zu bytes", scratch_bytes, need);
+  launch_select(dtype == DINFER_BF16, SelectArgs{d_logits, row_stride, n_seq, n_rows, vocab, n_keep, d_score, d_hold, d_row, d_token, d_score_out, d_scratch},
+                (hipStream_t)stream);
+  HIP_TRY(hipGetLastError());
+  return DINFER_OK;
+}
+
+static PagePool page_pool(const dinfer_ctx* c) {
+  return PagePool{c->kv, (int64_t)c->kv_layer_bytes, c->geom.page_stride * (c->bf16 ? 2 : 4), c->cfg.n_layers, c->n_pages};
+}
+static int check_pool(const dinfer_ctx* c) {
+  if (c->n_pages > MAX_POOL_PAGES) return fail(DINFER_EUNSUPPORTED, "%d pages, more than %d", c->n_pages, MAX_POOL_PAGES);
+  return check_device(c);
+}
+
+int dinfer_kv_fork(dinfer_ctx* c, int32_t n_old, int32_t n_new, const int32_t* d_parent, const int32_t* d_len, const int32_t* d_held,
+                   const int32_t* d_page_table, int32_t pt_stride, int32_t room, int32_t rewrite, const int32_t* d_refs,
+                   int32_t* d_new_len, int32_t* d_new_held, int32_t* d_new_page_table, int32_t new_pt_stride, int32_t* d_new_refs,
+                   int32_t* d_short, const dinfer_state* h_states, int32_t n_states, void* stream) {
+  if (!c) return fail(DINFER_EINVAL, "context is null");
+  if (!d_parent || !d_refs || !d_new_len || !d_new_held || !d_new_page_table || !d_new_refs || !d_short) return fail(DINFER_EINVAL, "null pointer");
+  if (n_old < 0 || n_old > c->max_seqs || n_new < 1 || n_new > c->max_seqs)
+    return fail(DINFER_EINVAL, "%d sequences out of %d, at most %d", n_new, n_old, c->max_seqs);
+  if (n_old > 0 && (!d_len || !d_held || !d_page_table || pt_stride < 1)) return fail(DINFER_EINVAL, "old sequences without lengths or page tables");
+  if (new_pt_stride < 1) return fail(DINFER_ENOSPACE, "page table row too short");
+  if (room < 0 || room > c->cfg.max_pos || rewrite < 0 || rewrite > c->cfg.max_pos) return fail(DINFER_EINVAL, "room %d, rewrite %d", room, rewrite);
+  if (d_new_refs == d_refs || d_new_page_table == d_page_table || d_new_len == d_len || d_new_held == d_held)
+    return fail(DINFER_EINVAL, "an output is an input");
+  if (n_states < 0 || n_states > MAX_STATES || (n_states > 0 && !h_states)) return fail(DINFER_EINVAL, "%d states", n_states);
+  ForkArgs a{};
+  int64_t groups = 2 * MAX_SEQS;
+  for (int k = 0; k < n_states; ++k) {
+    const dinfer_state& s = h_states[k];
+    if (!s.d_out || (!s.d_in && n_old > 0) || s.d_in == s.d_out) return fail(DINFER_EINVAL, "state %d: null, or in place", k);
+    if (s.row_bytes < 4 || s.row_bytes > INT32_MAX || (s.row_bytes | (uintptr_t)s.d_in | (uintptr_t)s.d_out) & 3)
+      return fail(DINFER_EINVAL, "state %d: rows of %lld bytes", k, (long long)s.row_bytes);
+    a.state[k] = StateRows{(const char*)s.d_in, (char*)s.d_out, s.row_bytes};
+    groups += (s.row_bytes / 4096 + 1) * n_new;
+  }
+  int rc = check_pool(c);
+  if (rc != DINFER_OK) return rc;
+  a.pool = page_pool(c);
+  groups += ((int64_t)rewrite / PAGE + 2) * n_new * a.pool.n_layers * (a.pool.page_bytes / 4096 + 1);
+  if (groups > INT32_MAX) return fail(DINFER_EUNSUPPORTED, "too many pages to copy in one call");
+  a.n_old = n_old, a.n_new = n_new;
+  a.parent = d_parent, a.len = d_len, a.held = d_held;
+  a.table = d_page_table, a.pt_stride = pt_stride;
+  int64_t limit = (int64_t)(pt_stride < new_pt_stride ? pt_stride : new_pt_stride) * PAGE;
+  if (n_old == 0) limit = 0;
+  a.limit = limit < c->cfg.max_pos ? (int32_t)limit : c->cfg.max_pos;
+  a.room = room, a.rewrite = rewrite;
+  a.refs = d_refs;
+  a.new_len = d_new_len, a.new_held = d_new_held, a.new_table = d_new_page_table, a.new_stride = new_pt_stride;
+  a.new_refs = d_new_refs, a.missing = d_short;
+  a.n_states = n_states;
+  launch_fork(a, (hipStream_t)stream);
+  HIP_TRY(hipGetLastError());
+  return DINFER_OK;
+}
+
+int dinfer_kv_compact(dinfer_ctx* c, int32_t n_seq, const int32_t* d_held, const int32_t* d_page_table, int32_t pt_stride,
+                      const int32_t* d_refs, int32_t* d_new_page_table, int32_t* d_new_refs, int32_t* d_moved, int32_t* d_count,
+                      void* stream) {
+  if (!c) return fail(DINFER_EINVAL, "context is null");
+  if (!d_held || !d_page_table || !d_refs || !d_new_page_table || !d_new_refs || !d_moved || !d_count) return fail(DINFER_EINVAL, "null pointer");
+  if (n_seq < 1 || n_seq > c->max_seqs) return fail(DINFER_EINVAL, "n_seq %d outside [1, %d]", n_seq, c->max_seqs);
+  if (pt_stride < 1) return fail(DINFER_ENOSPACE, "page table row too short");
+  if (d_new_page_table == d_page_table || d_new_refs == d_refs) return fail(DINFER_EINVAL, "an output is an input");
+  const int rc = check_pool(c);
+  if (rc != DINFER_OK) return rc;
+  launch_compact(CompactArgs{page_pool(c), n_seq, d_held, d_page_table, pt_stride, d_refs, d_new_page_table, d_new_refs, d_moved, d_count},
+                 (hipStream_t)stream);
   HIP_TRY(hipGetLastError());
   return DINFER_OK;
 }

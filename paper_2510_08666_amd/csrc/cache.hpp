@@ -70,6 +70,15 @@ struct AppendArgs {
 };
 void launch_append(bool bf16, const AppendArgs& a, hipStream_t st);
 
+// What the rows of an attention under a rule see (dinfer_attend_rule, its lengths brought into a cache's).
+struct AttendRule {
+  int32_t block, window;
+  const int32_t *prefix;      // [n_seq]
+  const int32_t *first, *end; // [T]
+  float cap;
+  const float* slope;         // [n_heads * group]
+};
+
 // Queries of one cache head's group are rows of one contraction: row r of a sequence is token r / group, query head
 // head * group + r % group.
 struct AttendArgs {
@@ -86,10 +95,13 @@ struct AttendArgs {
   float* lse;                 // [T][n_heads * group] natural logarithm of a row's sum of exponentials, or null
   float* part;                // attend_part_bytes
   bool whole;                 // set by the launch: no pair's keys are cut
+  AttendRule rule;            // launch_ruled
 };
 size_t attend_part_bytes(bool bf16, int head_dim, int max_pos);
 // planes: of the queries (two: the forward's own bfloat16 queries, normalisers only).
 void launch_attend(bool bf16, int planes, const AttendArgs& a, hipStream_t st);
+// Under a.rule (a.visible null).
+void launch_ruled(bool bf16, const AttendArgs& a, hipStream_t st);
 
 struct ScoreArgs {
   CacheTokens tok;
@@ -129,5 +141,6 @@ struct EvictArgs {
 void launch_evict(bool bf16, const EvictArgs& a, hipStream_t st);
 
 bool configure_attend();
+bool configure_ruled();
 
 }  // namespace dinfer
