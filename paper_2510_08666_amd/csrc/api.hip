@@ -1288,7 +1288,7 @@ static int check_select(int32_t n_seq, int32_t n_rows, int32_t vocab, int32_t n_
 }
 size_t dinfer_beam_scratch_bytes(int32_t n_seq, int32_t n_rows, int32_t vocab, int32_t n_keep) {
   if (check_select(n_seq, n_rows, vocab, n_keep) != DINFER_OK) return 0;
-  return select_scratch_bytes((int64_t)n_seq * n_rows, vocab, n_keep);
+  return select_scratch_bytes((int64_t)n_seq * n_rows, vocab);
 }
 int dinfer_beam_select(const void* d_logits, int32_t dtype, int64_t row_stride, int32_t n_seq, int32_t n_rows, int32_t vocab,
                        const float* d_score, const int32_t* d_hold, int32_t n_keep, int32_t* d_row, int32_t* d_token,
@@ -1300,7 +1300,7 @@ int dinfer_beam_select(const void* d_logits, int32_t dtype, int64_t row_stride, 
   if (row_stride < vocab || (uintptr_t)d_logits % (dtype == DINFER_BF16 ? 2 : 4)) return fail(DINFER_EINVAL, "rows %lld elements apart", (long long)row_stride);
   if (d_score_out == d_score || d_row == d_token) return fail(DINFER_EINVAL, "an output is another argument");
   if ((uintptr_t)d_scratch & 255) return fail(DINFER_EINVAL, "d_scratch must be 256-byte aligned");
-  const size_t need = select_scratch_bytes((int64_t)n_seq * n_rows, vocab, n_keep);
+  const size_t need = select_scratch_bytes((int64_t)n_seq * n_rows, vocab);
   if (scratch_bytes < need) return fail(DINFER_ENOSPACE, "scratch %zu < %zu bytes", scratch_bytes, need);
   launch_select(dtype == DINFER_BF16, SelectArgs{d_logits, row_stride, n_seq, n_rows, vocab, n_keep, d_score, d_hold, d_row, d_token, d_score_out, d_scratch},
                 (hipStream_t)stream);

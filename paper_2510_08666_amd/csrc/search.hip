@@ -5,14 +5,12 @@
 namespace dinfer {
 
 // ---------------------------------------------------------------- select
-// Candidates (row, token) with score[row] + z - log(sum of exp z) and the n_keep best of every sequence.  Within a row the order is that of
-// the logits, so the first launch, a workgroup per slice of a row, leaves the slice's n_keep best logits and its (maximum, sum of exponentials), and
-// the second one, a workgroup per sequence, the rows' normalisers and the best of what is left, in 64 bits.  Only what could be
-// among the best is sorted: the n_keep-th largest of the lanes' own maxima is no larger than the n_keep-th largest value.
+// Candidates (row, token) with score[row] + z - log(sum of exp z) and the n_keep best of every sequence.  The first launch streams the logits
+// once and leaves the maximum and the sum of exponentials of every chunk of 2048.  The second one, a workgroup per sequence, works
+// the rows' normalisers out of them, and a threshold: the n_keep-th best of the chunks' best candidates is no better than the n_keep-th
+// best candidate, so that only chunks that reach it, about n_keep of them, are read again, and what reaches it there is ranked, in 64 bits.
+constexpr int CHUNK_VALUES = 32, CHUNK = WAVE * CHUNK_VALUES;          // logits of a lane, in registers, and of a wave
 constexpr int SELECT_THREADS = 256, SELECT_WAVES = SELECT_THREADS / WAVE;
-constexpr int LANE_VALUES = 32;                                        // logits of a lane, in registers
-constexpr int SLICE = SELECT_THREADS * LANE_VALUES;
-constexpr int WAVE_LIST = 512;                                         // candidates of a wave that are ranked together
 constexpr uint32_t NO_VALUE = 0x007fffffu;                             // order_of(-inf): no candidate
 
 // Order of floats as integers; not a number counts as -inf.
@@ -20,150 +18,88 @@ __device__ inline uint32_t order_of(float v) {
   const uint32_t b = __float_as_uint(v + 0.f);
   return v != v ? NO_VALUE : b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
-__device__ inline float value_of(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o ^ 0x80000000u : ~o); }
-// Best first: the larger value, then the lower token.
-__device__ inline uint64_t key_of(uint32_t order, uint32_t token) { return (uint64_t)order << 32 | (uint32_t)~token; }
-__device__ inline uint32_t key_order(uint64_t k) { return (uint32_t)(k >> 32); }
-__device__ inline uint32_t key_token(uint64_t k) { return ~(uint32_t)k; }
 
-// The largest t of `bits` leading bits that at least `want` lanes reach.
-__device__ inline uint32_t reached_by(uint32_t order, int want, int bits) {
-  uint32_t t = 0;
-  for (int b = 31; b > 31 - bits; --b) {
-    const uint32_t up = t | 1u << b;
-    if (__popcll(__builtin_amdgcn_ballot_w64(order >= up)) >= want) t = up;
+struct ChunkState {
+  float m, s;                 // -inf: no candidate
+};
+static int select_chunks(int vocab) { return (vocab + CHUNK - 1) / CHUNK; }
+size_t select_scratch_bytes(int64_t rows, int vocab) { return rows * select_chunks(vocab) * sizeof(ChunkState); }
+
+// A lane's share of a chunk; -inf behind the row and where there is no number.  A lane's tokens are the same for every row, wherever
+// it begins in memory (the loads need not be aligned), so that equal rows have equal sums, to the bit, and tie.
+template <typename E> struct ChunkOf {
+  static constexpr int G = ET<E>::G, N = CHUNK_VALUES / G;
+  typename ET<E>::vec v[N];
+  __device__ static int token(int chunk, int lane, int r) { return chunk * CHUNK + (r / G * WAVE + lane) * G + r % G; }
+  __device__ void load(const E* z, int vocab, int chunk, int lane) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int at = token(chunk, lane, n * G);
+      if (at + G <= vocab) __builtin_memcpy(&v[n], z + at, sizeof(v[n]));
+      else
+#pragma unroll
+        for (int i = 0; i < G; ++i) v[n][i] = at + i < vocab ? z[at + i] : from_f32<E>(-INFINITY);
+    }
   }
-  return t;
+  __device__ float raw(int r) const { return to_f32(v[r / G][r % G]); }
+  __device__ float value(int r) const {
+    const float x = raw(r);
+    return x != x ? -INFINITY : x;
+  }
+};
+
+// Largest and sum over a wave, in every lane, by moves inside the registers up to rows of 16 lanes.
+template <int CTRL> __device__ inline float from_lane(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+__device__ inline float wave_largest(float v) {
+  v = fmaxf(v, from_lane<0x128>(v));      // row_ror:8, 4, 2, 1
+  v = fmaxf(v, from_lane<0x124>(v));
+  v = fmaxf(v, from_lane<0x122>(v));
+  v = fmaxf(v, from_lane<0x121>(v));
+  v = fmaxf(v, __shfl_xor(v, 16, WAVE));
+  return fmaxf(v, __shfl_xor(v, 32, WAVE));
+}
+__device__ inline float wave_total(float v) {
+  v += from_lane<0x128>(v);
+  v += from_lane<0x124>(v);
+  v += from_lane<0x122>(v);
+  v += from_lane<0x121>(v);
+  v += __shfl_xor(v, 16, WAVE);
+  return v + __shfl_xor(v, 32, WAVE);
 }
 
-struct SliceState {
-  float m, s;
-};
-struct SelectScratch {
-  SliceState* state;          // [row][slice]
-  uint64_t* key;              // [row][slice][n_keep], best first, 0 behind the last
-};
-static size_t state_bytes(int64_t lists) { return (lists * sizeof(SliceState) + 255) / 256 * 256; }
-static int select_slices(int vocab) { return (vocab + SLICE - 1) / SLICE; }
-static SelectScratch scratch_of(const SelectArgs& a) {
-  const int64_t lists = (int64_t)a.n_seq * a.n_rows * select_slices(a.vocab);
-  return SelectScratch{(SliceState*)a.scratch, (uint64_t*)((char*)a.scratch + state_bytes(lists))};
-}
-size_t select_scratch_bytes(int64_t rows, int vocab, int n_keep) {
-  const int64_t lists = rows * select_slices(vocab);
-  return state_bytes(lists) + lists * n_keep * sizeof(uint64_t);
-}
-
-template <typename E>
-__global__ __launch_bounds__(SELECT_THREADS) void select_slice_kernel(SelectArgs a, SelectScratch w) {
-  typedef typename ET<E>::vec vec;
-  constexpr int G = ET<E>::G, N = LANE_VALUES / G;
+// A wave takes PER chunks of a row, the next one's loads under way while it works on one.
+template <typename E, int PER>
+__global__ __launch_bounds__(SELECT_THREADS) void select_chunk_kernel(SelectArgs a, ChunkState* state, int chunks) {
   const int64_t row = blockIdx.y;
-  if (!(a.score[row] > -INFINITY) || (a.hold && a.hold[row] >= 0)) return;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, K = a.n_keep;
+  const int chunk0 = (blockIdx.x * SELECT_WAVES + (threadIdx.x >> 6)) * PER, lane = threadIdx.x & 63;
+  if (chunk0 >= chunks || !(a.score[row] > -INFINITY) || (a.hold && a.hold[row] >= 0)) return;
   const E* z = (const E*)a.logits + row * a.row_stride;
-  // A lane's tokens are the same for every row, wherever it begins in memory (the loads need not be aligned), so that equal rows have
-  // equal sums, to the bit, and tie.
-  const int first = (int)blockIdx.x * SLICE + wave * (WAVE * LANE_VALUES);
-  float x[LANE_VALUES];
+  ChunkOf<E> x, next;
+  x.load(z, a.vocab, chunk0, lane);
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const int at = first + (n * WAVE + lane) * G;
-    if (at + G <= a.vocab) {
-      vec v;
-      __builtin_memcpy(&v, z + at, sizeof(v));
+  for (int i = 0; i < PER; ++i) {
+    const int chunk = chunk0 + i;
+    if (i + 1 < PER && chunk + 1 < chunks) next.load(z, a.vocab, chunk + 1, lane);
+    float top = -INFINITY;
 #pragma unroll
-      for (int i = 0; i < G; ++i) x[n * G + i] = to_f32(v[i]);
-    } else {
+    for (int r = 0; r < CHUNK_VALUES; ++r) top = fmaxf(top, x.raw(r));      // (the larger of a number and NaN is the number)
+    const float M = wave_largest(top), shift = M > -INFINITY ? M * 1.44269504088896341f : 0.f;
+    float sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < G; ++i) x[n * G + i] = at + i < a.vocab ? to_f32(z[at + i]) : -INFINITY;
+    for (int r = 0; r < CHUNK_VALUES; ++r) sum += __builtin_amdgcn_exp2f(fmaf(x.raw(r), 1.44269504088896341f, -shift));
+    sum = wave_total(sum);
+    if (!(sum < INFINITY)) {      // NaN among them, or infinities, which count one each
+      sum = 0.f;
+#pragma unroll
+      for (int r = 0; r < CHUNK_VALUES; ++r)
+        sum += M < INFINITY ? __builtin_amdgcn_exp2f(fmaf(x.value(r), 1.44269504088896341f, -shift)) : x.value(r) == M ? 1.f : 0.f;
+      sum = wave_total(sum);
     }
-  }
-  auto token_at = [&](int r) { return first + (r / G * WAVE + lane) * G + r % G; };
-  float top = -INFINITY;
-#pragma unroll
-  for (int r = 0; r < LANE_VALUES; ++r) {
-    x[r] = x[r] != x[r] ? -INFINITY : x[r];
-    top = fmaxf(top, x[r]);
-  }
-  const float M = wave_max(top);
-  float sum = 0.f;
-#pragma unroll
-  for (int r = 0; r < LANE_VALUES; ++r) sum += x[r] == M ? 1.f : __builtin_amdgcn_exp2f((x[r] - M) * 1.44269504088896341f);
-  sum = M > -INFINITY ? wave_sum(sum) : 0.f;
-
-  __shared__ uint64_t list[SELECT_WAVES][WAVE_LIST];
-  __shared__ uint64_t best[SELECT_WAVES][MAX_KEEP];
-  __shared__ SliceState state[SELECT_WAVES];
-  if (lane == 0) state[wave] = SliceState{M, sum};
-  const uint32_t least = max(reached_by(order_of(top), K, 20), NO_VALUE + 1);
-  int n = 0;
-  const uint64_t below = lane ? ~0ull >> (64 - lane) : 0ull;
-#pragma unroll
-  for (int r = 0; r < LANE_VALUES; ++r) {
-    const uint32_t o = order_of(x[r]);
-    const uint64_t in = __builtin_amdgcn_ballot_w64(o >= least);
-    const int at = n + __popcll(in & below);
-    if (o >= least && at < WAVE_LIST) list[wave][at] = key_of(o, token_at(r));
-    n += __popcll(in);
-  }
-  if (lane < K) best[wave][lane] = 0;
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  if (n <= WAVE_LIST) {
-    for (int i = lane; i < n; i += WAVE) {
-      const uint64_t mine = list[wave][i];
-      int rank = 0;
-      for (int j = 0; j < n; ++j) rank += list[wave][j] > mine;
-      if (rank < K) best[wave][rank] = mine;
-    }
-  } else {
-    // hundreds of equal values: one after the other
-    uint64_t last = ~0ull;
-    for (int k = 0; k < K; ++k) {
-      uint64_t mine = 0;
-#pragma unroll
-      for (int r = 0; r < LANE_VALUES; ++r) {
-        const uint32_t o = order_of(x[r]);
-        const uint64_t key = o > NO_VALUE ? key_of(o, token_at(r)) : 0;
-        mine = key < last && key > mine ? key : mine;
-      }
-#pragma unroll
-      for (int d = 32; d > 0; d >>= 1) {
-        const uint64_t other = __shfl_xor((unsigned long long)mine, d, WAVE);
-        mine = other > mine ? other : mine;
-      }
-      if (mine == 0) break;
-      if (lane == 0) best[wave][k] = mine;
-      last = mine;
-    }
-  }
-  __syncthreads();
-  // the waves' lists joined
-  const int64_t unit = row * gridDim.x + blockIdx.x;
-  uint64_t* out = w.key + unit * K;
-  __shared__ int filled;
-  if (threadIdx.x == 0) filled = 0;
-  __syncthreads();
-  for (int i = threadIdx.x; i < SELECT_WAVES * K; i += SELECT_THREADS) {
-    const uint64_t mine = best[i / K][i % K];
-    if (mine == 0) continue;
-    int rank = 0;
-    for (int v = 0; v < SELECT_WAVES; ++v)
-      for (int j = 0; j < K; ++j) rank += best[v][j] > mine;
-    if (rank < K) {
-      out[rank] = mine;
-      atomicAdd(&filled, 1);
-    }
-  }
-  __syncthreads();
-  for (int i = filled + threadIdx.x; i < K; i += SELECT_THREADS) out[i] = 0;
-  if (threadIdx.x == 0) {
-    float top_m = -INFINITY, s = 0.f;
-    for (int v = 0; v < SELECT_WAVES; ++v) top_m = fmaxf(top_m, state[v].m);
-    for (int v = 0; v < SELECT_WAVES; ++v)
-      s += state[v].m == top_m ? state[v].s : state[v].s * __builtin_amdgcn_exp2f((state[v].m - top_m) * 1.44269504088896341f);
-    w.state[unit] = SliceState{top_m, top_m > -INFINITY ? s : 0.f};
+    if (lane == 0) state[row * chunks + chunk] = ChunkState{M, sum};
+    if (chunk + 1 >= chunks) return;
+    x = next;
   }
 }
 
@@ -174,99 +110,208 @@ struct Candidate {
 };
 __device__ inline bool better(const Candidate& x, const Candidate& y) { return x.score > y.score || (x.score == y.score && x.at < y.at); }
 
-constexpr int JOIN_THREADS = 1024, JOIN_WAVES = JOIN_THREADS / WAVE, JOIN_LIST = 2048;
-__global__ __launch_bounds__(JOIN_THREADS) void select_join_kernel(SelectArgs a, SelectScratch w, int slices) {
-  const int seq = blockIdx.x, wave = threadIdx.x >> 6, lane = threadIdx.x & 63, K = a.n_keep, R = a.n_rows;
+constexpr int JOIN_THREADS = 1024, JOIN_WAVES = JOIN_THREADS / WAVE;
+constexpr int JOIN_CHUNKS = 1024, JOIN_LIST = 2048;                    // chunks that are read again, candidates that are ranked together
+constexpr int JOIN_ROWS = 4;                                           // rows of a wave whose chunks are under way together
+template <typename E>
+__global__ __launch_bounds__(JOIN_THREADS) void select_join_kernel(SelectArgs a, const ChunkState* state, int chunks) {
+  const int seq = blockIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, K = a.n_keep, R = a.n_rows;
   const int64_t row0 = (int64_t)seq * R;
-  __shared__ double norm[MAX_SELECT_ROWS];      // score - log(sum of exp z); for rows that hold: the score
+  state += row0 * chunks;
+  __shared__ double norm[MAX_SELECT_ROWS];      // score - log(sum of exp z); of rows that hold: the score
   __shared__ float peak[MAX_SELECT_ROWS];       // largest logit of the row, -inf: no candidate, NaN: one that is held
-  for (int r = wave; r < R; r += JOIN_WAVES) {
-    const float base = a.score[row0 + r];
-    const bool live = base > -INFINITY, held = live && a.hold && a.hold[row0 + r] >= 0;
-    float M = -INFINITY;
-    double s = 0.0;
-    if (live && !held) {
-      const SliceState* st = w.state + (row0 + r) * slices;
-      for (int i = lane; i < slices; i += WAVE) M = fmaxf(M, st[i].m);
-      M = wave_max(M);
-      for (int i = lane; i < slices; i += WAVE)
-        if (st[i].m > -INFINITY) s += st[i].m == M ? (double)st[i].s : (double)st[i].s * exp((double)st[i].m - (double)M);
-#pragma unroll
-      for (int d = 32; d > 0; d >>= 1) s += __shfl_xor(s, d, WAVE);
-    }
-    if (lane == 0) {
-      peak[r] = held ? __builtin_nanf("") : M;
-      // (infinite logits share the row's weight: log(1 / their number) each)
-      norm[r] = held ? (double)base : M > -INFINITY ? (double)base - ((M < INFINITY ? (double)M : 0.0) + log(s)) : 0.0;
-    }
-  }
-  __shared__ Candidate list[JOIN_LIST];
-  __shared__ int n_list;
-  __shared__ uint32_t reach[JOIN_WAVES];
-  if (threadIdx.x == 0) n_list = 0;
-  __syncthreads();
-  const int lists = R * slices;
-  // candidate k of a list; false: there is none
-  auto look = [&](int l, int k, Candidate& c) {
-    const int r = l / slices;
-    const float p = peak[r];
-    if (p != p) {
-      c = Candidate{norm[r], (uint64_t)r << 32 | (uint32_t)a.hold[row0 + r]};
-      return l % slices == 0 && k == 0;
-    }
-    if (!(p > -INFINITY)) return false;
-    const uint64_t key = w.key[(row0 * slices + l) * K + k];
-    const float z = value_of(key_order(key));
-    c = Candidate{norm[r] + (p < INFINITY ? (double)z : 0.0), (uint64_t)r << 32 | key_token(key)};
-    return key != 0 && (p < INFINITY || z == INFINITY);
+  __shared__ float row_sum[MAX_SELECT_ROWS];
+  __shared__ __align__(16) Candidate list[JOIN_LIST];
+  __shared__ int chunk_row[JOIN_CHUNKS], chunk_at[JOIN_CHUNKS];
+  __shared__ int n_list, n_chunks, n_top;
+  __shared__ uint32_t reach[JOIN_WAVES], least_of_all;
+  uint32_t* tops = reinterpret_cast<uint32_t*>(list);      // (before the list is used)
+  static_assert(sizeof(list) >= JOIN_THREADS * sizeof(uint32_t), "a value per thread");
+  if (threadIdx.x == 0) n_list = n_chunks = n_top = 0;
+  // the best candidate's score of a chunk with the largest logit m, rounded to a float (-inf: none)
+  auto head = [](double n, float p, float m, bool first) {
+    if (p != p) return first ? (float)n : -INFINITY;
+    if (!(p > -INFINITY) || !(m > -INFINITY)) return -INFINITY;
+    return p < INFINITY ? (float)(n + (double)m) : m == INFINITY ? (float)n : -INFINITY;
   };
-  // no candidate below the K-th largest first one of any wave's lanes is wanted (scores as floats, rounded: what is as large, is looked at)
+  // A batch of rows: maximum and sum of each (a wave has JOIN_ROWS of them), the normalisers a lane per row, then the chunks' best.
   float top = -INFINITY;
-  for (int l = threadIdx.x; l < lists; l += JOIN_THREADS) {
-    Candidate c;
-    if (look(l, 0, c)) top = fmaxf(top, (float)c.score);
-  }
-  const uint32_t t = reached_by(order_of(top), K, 32);
-  if (lane == 0) reach[wave] = t;
-  __syncthreads();
-  uint32_t least = NO_VALUE;
-  for (int v = 0; v < JOIN_WAVES; ++v) least = max(least, reach[v]);
-  for (int l = threadIdx.x; l < lists; l += JOIN_THREADS)
-    for (int k = 0; k < K; ++k) {
-      Candidate c;
-      if (!look(l, k, c) || order_of((float)c.score) < least) break;
-      const int at = atomicAdd(&n_list, 1);
-      if (at < JOIN_LIST) list[at] = c;
+  for (int b0 = 0; b0 < R; b0 += JOIN_WAVES * JOIN_ROWS) {
+    const int r0 = b0 + wave;
+    float M[JOIN_ROWS], s[JOIN_ROWS];
+#pragma unroll
+    for (int u = 0; u < JOIN_ROWS; ++u) M[u] = -INFINITY, s[u] = 0.f;
+    const int mine = min(b0 + (int)threadIdx.x, R - 1);
+    const float base = a.score[row0 + mine];
+    const int hold = *(a.hold ? a.hold + row0 + mine : a.row);      // (some readable word)
+    for (int c0 = 0; c0 < chunks; c0 += 2 * WAVE) {
+      ChunkState st[JOIN_ROWS][2];
+#pragma unroll
+      for (int u = 0; u < JOIN_ROWS; ++u)
+#pragma unroll
+        for (int v = 0; v < 2; ++v)      // (of rows that take no part: anything)
+          st[u][v] = state[(int64_t)min(r0 + u * JOIN_WAVES, R - 1) * chunks + min(c0 + v * WAVE + lane, chunks - 1)];
+#pragma unroll
+      for (int u = 0; u < JOIN_ROWS; ++u)
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          const bool is = c0 + v * WAVE + lane < chunks && st[u][v].m > -INFINITY;
+          const float m = is ? st[u][v].m : -INFINITY, both = fmaxf(M[u], m);
+          const float keep = M[u] == both ? 1.f : __builtin_amdgcn_exp2f((M[u] - both) * 1.44269504088896341f);
+          const float take = m == both ? 1.f : __builtin_amdgcn_exp2f((m - both) * 1.44269504088896341f);
+          s[u] = s[u] * keep + (is ? st[u][v].s * take : 0.f);
+          M[u] = both;
+        }
     }
+#pragma unroll
+    for (int u = 0; u < JOIN_ROWS; ++u) {
+      const float p = wave_largest(M[u]);
+      const float sum = wave_total(M[u] == p ? s[u] : s[u] * __builtin_amdgcn_exp2f((M[u] - p) * 1.44269504088896341f));
+      if (lane == 0 && r0 + u * JOIN_WAVES < R) {
+        peak[r0 + u * JOIN_WAVES] = p;
+        row_sum[r0 + u * JOIN_WAVES] = sum;
+      }
+    }
+    __syncthreads();
+    if (threadIdx.x < JOIN_WAVES * JOIN_ROWS && b0 + (int)threadIdx.x < R) {
+      const float p = peak[mine];
+      const bool live = base > -INFINITY, held = live && a.hold && hold >= 0, some = live && !held && p > -INFINITY;
+      peak[mine] = held ? __builtin_nanf("") : some ? p : -INFINITY;
+      // (infinite logits share the row's weight: log(1 / their number) each)
+      norm[mine] = held ? (double)base : some ? (double)base - ((p < INFINITY ? (double)p : 0.0) + log((double)row_sum[mine])) : 0.0;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < JOIN_ROWS; ++u) {
+      const int r = r0 + u * JOIN_WAVES;
+      if (r < R) top = fmaxf(top, head(norm[r], peak[r], M[u], lane == 0));
+    }
+  }
+  // the K-th largest of the threads' best ones, or a little less: a bound from below by every wave's own, then among those that reach it
+  {
+    const uint32_t mine = order_of(top);
+    uint32_t t = 0;
+    for (int b = 31; b >= 16; --b) {
+      const uint32_t up = t | 1u << b;
+      if (__popcll(__builtin_amdgcn_ballot_w64(mine >= up)) >= K) t = up;
+    }
+    if (lane == 0) reach[wave] = t;
+    __syncthreads();
+    t = 0;
+#pragma unroll
+    for (int v = 0; v < JOIN_WAVES; ++v) t = max(t, reach[v]);
+    if (mine >= t && mine > NO_VALUE) tops[atomicAdd(&n_top, 1)] = mine;
+    __syncthreads();
+    if (wave == 0) {
+      constexpr int U = 4;
+      const int n = n_top;
+      if (n >= K && n <= U * WAVE) {
+        uint32_t x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = u * WAVE + lane < n ? tops[u * WAVE + lane] : 0;
+        t = 0;
+        for (int b = 31; b >= 10; --b) {
+          const uint32_t up = t | 1u << b;
+          int reached = 0;
+#pragma unroll
+          for (int u = 0; u < U; ++u) reached += __popcll(__builtin_amdgcn_ballot_w64(x[u] >= up));
+          if (reached >= K) t = up;
+        }
+      }
+      if (lane == 0) least_of_all = max(t, NO_VALUE + 1);
+    }
+    __syncthreads();
+  }
+  const uint32_t least = least_of_all;
+  // every chunk whose best candidate reaches it
+  auto each_chunk = [&](auto use) {
+    for (int r0 = wave; r0 < R; r0 += JOIN_WAVES * JOIN_ROWS)
+      for (int c0 = 0; c0 < chunks; c0 += WAVE) {
+        float m[JOIN_ROWS];
+#pragma unroll
+        for (int u = 0; u < JOIN_ROWS; ++u) m[u] = state[(int64_t)min(r0 + u * JOIN_WAVES, R - 1) * chunks + min(c0 + lane, chunks - 1)].m;
+#pragma unroll
+        for (int u = 0; u < JOIN_ROWS; ++u) {
+          const int r = r0 + u * JOIN_WAVES;
+          if (r < R) use(r, c0, c0 + lane < chunks && order_of(head(norm[r], peak[r], m[u], c0 + lane == 0)) >= least);
+        }
+      }
+  };
+  each_chunk([&](int r, int c0, bool reaches) {
+    if (reaches) {
+      const int at = atomicAdd(&n_chunks, 1);
+      if (at < JOIN_CHUNKS) {
+        chunk_row[at] = r;
+        chunk_at[at] = c0 + lane;
+      }
+    }
+  });
   __syncthreads();
-  const int n = n_list;
   const int64_t out = (int64_t)seq * K;
   auto put = [&](int k, const Candidate& c) {
     a.row[out + k] = (int32_t)(c.at >> 32);
     a.token[out + k] = (int32_t)c.at;
     a.score_out[out + k] = (float)c.score;
   };
-  int filled = n;
-  if (n <= JOIN_LIST) {
+  const double bound = (double)__uint_as_float(least & 0x80000000u ? least ^ 0x80000000u : ~least);
+  // the candidates of a chunk that reach it, in this wave
+  auto scan = [&](int r, int chunk, auto take) {
+    const float p = peak[r];
+    const double n = norm[r];
+    if (p != p) {
+      if (lane == 0) take(Candidate{n, (uint64_t)r << 32 | (uint32_t)a.hold[row0 + r]});
+      return;
+    }
+    ChunkOf<E> x;
+    x.load((const E*)a.logits + (row0 + r) * a.row_stride, a.vocab, chunk, lane);
+    // (a logit below `cut` cannot; those above it are looked at)
+    const float cut = p < INFINITY ? (float)(bound - n - (fabs(bound) + fabs(n) + 1.0) * 0x1p-20) : INFINITY;
+#pragma unroll
+    for (int v = 0; v < CHUNK_VALUES; ++v) {
+      const float z = x.value(v);
+      if (z >= cut && z > -INFINITY) {
+        const double score = p < INFINITY ? n + (double)z : n;
+        if (order_of((float)score) >= least) take(Candidate{score, (uint64_t)r << 32 | (uint32_t)ChunkOf<E>::token(chunk, lane, v)});
+      }
+    }
+  };
+  if (n_chunks <= JOIN_CHUNKS) {
+    for (int i = wave; i < n_chunks; i += JOIN_WAVES)
+      scan(__builtin_amdgcn_readfirstlane(chunk_row[i]), __builtin_amdgcn_readfirstlane(chunk_at[i]), [&](const Candidate& c) {
+        const int at = atomicAdd(&n_list, 1);
+        if (at < JOIN_LIST) list[at] = c;
+      });
+  }
+  __syncthreads();
+  const int n = n_list;
+  int filled = min(n, K);
+  if (n_chunks <= JOIN_CHUNKS && n <= JOIN_LIST) {
     for (int i = threadIdx.x; i < n; i += JOIN_THREADS) {
       const Candidate mine = list[i];
       int rank = 0;
-      for (int j = 0; j < n; ++j) rank += better(list[j], mine);
+      constexpr int U = 8;
+      for (int j0 = 0; j0 < n; j0 += U) {
+        Candidate c[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) c[u] = list[min(j0 + u, n - 1)];
+#pragma unroll
+        for (int u = 0; u < U; ++u) rank += j0 + u < n && better(c[u], mine);
+      }
       if (rank < K) put(rank, mine);
     }
   } else {
-    // thousands of equal scores: one after the other
+    // thousands of candidates reach the threshold, as equal ones do: the best one behind the last, K times
     __shared__ Candidate found[JOIN_WAVES];
     Candidate last{INFINITY, 0};
     bool begun = false;
     for (filled = 0; filled < K; ++filled) {
       Candidate mine{-INFINITY, ~0ull};
-      for (int l = threadIdx.x; l < lists; l += JOIN_THREADS)
-        for (int k = 0; k < K; ++k) {
-          Candidate c;
-          if (!look(l, k, c)) break;
-          if ((!begun || better(last, c)) && better(c, mine)) mine = c;
-        }
+      each_chunk([&](int r, int c0, bool reaches) {
+        for (uint64_t left = __builtin_amdgcn_ballot_w64(reaches); left; left &= left - 1)
+          scan(r, c0 + __builtin_ctzll(left), [&](const Candidate& c) {
+            if ((!begun || better(last, c)) && better(c, mine)) mine = c;
+          });
+      });
 #pragma unroll
       for (int d = 32; d > 0; d >>= 1) {
         const Candidate other{__shfl_xor(mine.score, d, WAVE), __shfl_xor((unsigned long long)mine.at, d, WAVE)};
@@ -283,19 +328,24 @@ __global__ __launch_bounds__(JOIN_THREADS) void select_join_kernel(SelectArgs a,
       begun = true;
     }
   }
-  for (int k = min(filled, K) + threadIdx.x; k < K; k += JOIN_THREADS) {
+  for (int k = filled + threadIdx.x; k < K; k += JOIN_THREADS) {
     a.row[out + k] = a.token[out + k] = -1;
     a.score_out[out + k] = -INFINITY;
   }
 }
 
+constexpr int SELECT_MANY = 4 * 8192;
+template <typename E> static void launch_select_t(const SelectArgs& a, hipStream_t st) {
+  const int chunks = select_chunks(a.vocab);
+  ChunkState* state = (ChunkState*)a.scratch;
+  const int64_t rows = (int64_t)a.n_seq * a.n_rows;
+  if (rows * chunks >= SELECT_MANY) select_chunk_kernel<E, 4><<<dim3((chunks + 4 * SELECT_WAVES - 1) / (4 * SELECT_WAVES), rows), SELECT_THREADS, 0, st>>>(a, state, chunks);
+  else select_chunk_kernel<E, 1><<<dim3((chunks + SELECT_WAVES - 1) / SELECT_WAVES, rows), SELECT_THREADS, 0, st>>>(a, state, chunks);
+  select_join_kernel<E><<<a.n_seq, JOIN_THREADS, 0, st>>>(a, state, chunks);
+}
 void launch_select(bool bf16, const SelectArgs& a, hipStream_t st) {
-  const SelectScratch w = scratch_of(a);
-  const int slices = select_slices(a.vocab);
-  const dim3 grid(slices, a.n_seq * a.n_rows);
-  if (bf16) select_slice_kernel<bf16_t><<<grid, SELECT_THREADS, 0, st>>>(a, w);
-  else select_slice_kernel<float><<<grid, SELECT_THREADS, 0, st>>>(a, w);
-  select_join_kernel<<<a.n_seq, JOIN_THREADS, 0, st>>>(a, w, slices);
+  if (bf16) launch_select_t<bf16_t>(a, st);
+  else launch_select_t<float>(a, st);
 }
 
 // ---------------------------------------------------------------- pages

@@ -20,7 +20,7 @@ struct SelectArgs {
   float* score_out;
   void* scratch;              // select_scratch_bytes
 };
-size_t select_scratch_bytes(int64_t rows, int vocab, int n_keep);
+size_t select_scratch_bytes(int64_t rows, int vocab);
 void launch_select(bool bf16, const SelectArgs& a, hipStream_t st);
 
 // The page pool and the counts of the sequences that hold each page.

@@ -18,7 +18,7 @@ def test_null_contexts():
 
 def test_select():
     size = b.lib.dinfer_beam_scratch_bytes
-    assert size(1, 1, 1, 1) > 0 and size(8, 64, 157184, 16) >= 8 * 64 * 20 * (16 * 8 + 8) and size(63, 1024, 100, 64) > 0
+    assert size(1, 1, 1, 1) > 0 and size(8, 64, 157184, 16) >= 8 * 64 * 77 * 8 and size(63, 1024, 100, 64) > 0
     for bad in ((0, 1, 1, 1), (1, 0, 1, 1), (1, 1025, 1, 1), (64, 1024, 1, 1), (1, 1, 0, 1), (1, 1, (1 << 24) + 1, 1), (1, 1, 1, 0), (1, 1, 1, 65)):
         assert size(*bad) == 0 and b.last_error() != "", bad
     good = [0x1000, b.F32, 9, 1, 2, 9, 0x2000, None, 3, 0x3000, 0x4000, 0x5000, 0x6000, 1 << 20, None]
