@@ -354,6 +354,15 @@ __device__ inline Piece piece_at(const Plan& p, uint32_t i, int n_heads) {
   c.cut = __builtin_amdgcn_readlane(p.cut_end, at_lane) - behind;
   return c;
 }
+// The same with the heads of a pair's part next to each other, so that each die, to which a launch's workgroups are dealt in turn, reads the keys of
+// few heads, and the last rows, which see the most of a causal sequence, first.
+__device__ inline Piece piece_by_heads(const Plan& p, uint32_t i, int n_heads) {
+  const int at_lane = __builtin_ctzll(__builtin_amdgcn_ballot_w64(p.end > i));
+  const uint32_t groups = __builtin_amdgcn_readlane(p.groups, at_lane), parts = __builtin_amdgcn_readlane(p.parts, at_lane);
+  const uint32_t first = __builtin_amdgcn_readlane(p.end, at_lane) - groups * n_heads * parts, at = (i - first) / n_heads;
+  // (its number in the order of piece_at: heads, in them parts, in those row groups)
+  return piece_at(p, first + ((i - first) % n_heads * parts + at % parts) * groups + groups - 1 - at / parts, n_heads);
+}
 // What the host sizes grids and partial results by.  Every pair that is cut has more than `per` tiles, and per * resident covers all
 // tiles: fewer than `resident` pairs are cut, into ceil(tiles / per) < 2 * tiles / per parts each, fewer than
 // 2 * resident in all; all workgroups are fewer than `resident` and one more per pair.
@@ -412,7 +421,9 @@ __global__ __launch_bounds__(ATTEND_WAVES * WAVE, (attend_waves_per_simd<E, HD>(
   const uint32_t wg = near_workgroup();
   if (wg >= plan.total) return;
   const Piece c = piece_at(plan, wg, a.geom.n_heads);
-  const int tile0 = Rule::first_tile(a, c.base), kt0 = tile0 + c.n_tiles * c.part / c.parts, kt1 = tile0 + c.n_tiles * (c.part + 1) / c.parts;
+  // (a part of a walk may lie anywhere in the sequence)
+  const int kt0 = Rule::RANGES ? Rule::first_tile(a, c.base) : c.n_tiles * c.part / c.parts;
+  const int kt1 = Rule::RANGES ? kt0 + c.n_tiles : c.n_tiles * (c.part + 1) / c.parts;
   const int tok0 = a.tok.span.off[c.seq], row0 = c.group * ROWS, n_rows = (a.tok.span.off[c.seq + 1] - tok0) * a.group - row0;      // rows from this group on: >= 1
   const int n_keys = c.base + a.tok.span.off[c.seq + 1] - tok0, last_page = (n_keys - 1) / PAGE - 2 * kt0, last_tile = kt1 - 1;
   const int row = row0 + min(rt * TILE + col, n_rows - 1), tok = tok0 + row / a.group, q_head = c.head * a.group + row % a.group;
@@ -555,9 +566,10 @@ __global__ __launch_bounds__(ATTEND_WAVES * WAVE, (attend_waves_per_simd<E, HD>(
     }
   };
   if constexpr (Rule::RANGES) {
-    const int n = rule.walk.tiles(), whole = rule.walk.whole();
-    if (team < n && rt * TILE < n_rows) {
-      int i = team, kt = rule.walk.tile(i);
+    const int all = rule.walk.tiles(), n = all * (c.part + 1) / c.parts, whole = min(n, rule.walk.whole());
+    int i = all * c.part / c.parts + team;
+    if (i < n && rt * TILE < n_rows) {
+      int kt = rule.walk.tile(i);
       load_k(kt);
       load_v(kt);
       auto walk = [&](int end, auto tail) {

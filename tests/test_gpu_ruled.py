@@ -241,3 +241,51 @@ def test_refusals(m):
     torch.cuda.synchronize()
     assert (out == 5).all()
     c.close()
+
+
+@pytest.mark.parametrize("dtype,nh,hd,G,lens,past,rule_name", [
+    ("bf16", 16, 128, 1, [1100, 40, 0, 900], [300, 1500, 7, 0], "causal"), ("bf16", 8, 128, 4, [700, 333], [0, 1000], "block7"),
+    ("bf16", 8, 64, 4, [1200, 900], [77, 500], "prefix_block"), ("bf16", 4, 128, 8, [600, 500], [900, 0], "all"),
+    ("bf16", 16, 128, 1, [2000, 1900], [0, 31], "documents"), ("bf16", 16, 128, 2, [800], [100], "prefix_window")])
+def test_the_form_of_many_rows(m, dtype, nh, hd, G, lens, past, rule_name):
+    """Calls that are large enough for it: a few tokens of them against the definition."""
+    cache, ops = m
+    c = cache.Cache(dtype, nh, hd, lens, past, seed=5, room=2000)
+    rule = make_rule(rule_name, lens, past, nh * G)
+    if "first" in rule:
+        rule.update(documents(lens, past, 613))
+    if rule.get("window"):
+        rule["window"] = 700
+    q, out, lse = c.randn(c.T, nh * G * hd, scale=1.5), torch.full((c.T + 1, nh * G * hd), 3.0, dtype=cache.TYPE[dtype], device=DEV), torch.zeros(c.T, nh * G, device=DEV)
+    odd = past[0] + lens[0] // 2
+    c.set_rows(0, [odd], v=torch.full((1, nh, hd), math.inf))
+    attend(c, q, out, rule, lse)
+    assert (out[c.T:] == 3).all()
+    # a sequence of the chosen tokens only: each a sequence of its own behind the same pages
+    t0 = 0
+    for s, (n, p) in enumerate(zip(lens, past)):
+        for i in sorted({0, 1, n // 3, n // 2, n // 2 + 1, n - 31, n - 1}):
+            if not 0 <= i < n:
+                continue
+            ok = ops.seen(rule, s, t0 + i, p + i, p + n)
+            k, v = c.rows(s, p + n)
+            at = torch.arange(p + n)
+            for h in (0, nh * G - 1):
+                z = k[:, h // G] @ q[t0 + i].cpu().double().view(-1, hd)[h] / math.sqrt(hd)
+                size = k[:, h // G].abs() @ q[t0 + i].cpu().double().view(-1, hd)[h].abs() / math.sqrt(hd)
+                e = float(size.max()) * (hd + 4) * 2.0 ** -24 + rule.get("cap", 0.0) * 2.0 ** -21
+                if rule.get("cap"):
+                    z = rule["cap"] * torch.tanh(z / rule["cap"])
+                if rule.get("slope") is not None:
+                    z = z - rule["slope"][h] * (at - p - i).abs()
+                    e += abs(rule["slope"][h]) * (p + n) * 2.0 ** -22
+                w = torch.softmax(z[ok], 0)
+                ref, mag = w @ v[ok, h // G], w @ v[ok, h // G].abs()
+                got = out[t0 + i].cpu().double().view(-1, hd)[h]
+                e = 2 * e + 2.0 ** -19
+                bar = 2.0 ** -8 * ref.abs() + (2.0 ** -8 + e) * mag
+                assert (((got - ref).abs() <= bar) | (got == ref)).all(), (s, i, h, float((got - ref).abs().max()))
+                norm = float(torch.logsumexp(z[ok], 0))
+                assert abs(float(lse[t0 + i, h]) - norm) <= e + 2.0 ** -21 * abs(norm)
+        t0 += n
+    c.close()
