@@ -588,14 +588,15 @@ class Context:
         i32 = torch.int32
         n_new, new_columns = self._sizes("d_new_page_table", d_new_page_table, 2)
         n_old, columns = (0, 0) if d_page_table is None else self._sizes("d_page_table", d_page_table, 2)
-        rows = (State * max(len(states), 1))()
+        rows = (State * len(states))() if states else None
         for k, (a, b) in enumerate(states):
-            for name, t, n in (("state %d" % k, a, n_old), ("new state %d" % k, b, n_new)):
-                if t.get_device() != self._index or not t.is_contiguous() or t.dim() < 1 or t.shape[0] < n:
-                    raise ValueError("%s must be a contiguous tensor of %d rows on the context's device" % (name, n))
-            if a.dtype is not b.dtype or a.shape[1:] != b.shape[1:]:
-                raise ValueError("state %d: rows of one type and size" % k)
-            rows[k] = State(a.data_ptr(), b.data_ptr(), b[:1].numel() * b.element_size())
+            sa, sb = a.shape, b.shape
+            if not (len(sa) > 0 and sa[1:] == sb[1:] and sa[0] >= n_old and sb[0] >= n_new and a.dtype is b.dtype and a.get_device() == self._index and
+                    b.get_device() == self._index and a.is_contiguous() and b.is_contiguous()):
+                raise ValueError("state %d must be two contiguous tensors on the context's device, a row of one type and size for each of %d old "
+                                 "and %d new sequences" % (k, n_old, n_new))
+            r = rows[k]
+            r.d_in, r.d_out, r.row_bytes = a.data_ptr(), b.data_ptr(), b.numel() // sb[0] * b.element_size()
         _check(lib.dinfer_kv_fork(self.h, n_old, n_new, self._flat("parent", parent, i32, n_new), self._flat("d_len", d_len, i32, n_old),
                                   self._flat("d_held", d_held, i32, n_old), self._flat("d_page_table", d_page_table, i32, n_old, columns), columns,
                                   room, rewrite, self._flat("refs", refs, i32, self.n_pages), self._flat("d_new_len", d_new_len, i32, n_new),

@@ -143,7 +143,7 @@ int attn_splits(int n_qtiles, int n_heads, int key_bound) {
 struct Workspace {
   size_t cos_tab, sin_tab, tok_seq, tok_pos, seq_nkeys, qtile, x, xn, xn_hi, ssq, ssq_a, tk_part, tickets, tickets_bytes, attn_tickets, attn_tickets_bytes, rinv_f, q, a, attn_part, topk_idx, topk_w, cnt, off,
       perm, shares, work, hist, run_tokens, run_base, n_finished, loop_flags, loop_steps, lm_rows, y, o, lm_part, smooth_part, lm_stats, conf, argmax,
-      tok_rot, attend_part, score_lse, total;
+      tok_rot, attend_part, score_lse, fork_copies, total;
 };
 
 Workspace map_workspace(const dinfer_config& c, int max_seqs, int max_tokens) {
@@ -219,6 +219,7 @@ Workspace map_workspace(const dinfer_config& c, int max_seqs, int max_tokens) {
   w.tok_rot = cv.take(T * 4);                    // rotary positions of a forward over a shortened cache
   w.attend_part = cv.take(attend_part_bytes(c.dtype == DINFER_BF16, c.head_dim, c.max_pos));
   w.score_lse = cv.take(T * c.n_heads * 4);      // normalisers of a scored step's rows
+  w.fork_copies = cv.take(fork_copies_bytes(max_seqs, c.max_pos));
   w.total = cv.at;
   return w;
 }
@@ -1356,6 +1357,7 @@ int dinfer_kv_fork(dinfer_ctx* c, int32_t n_old, int32_t n_new, const int32_t* d
   a.new_len = d_new_len, a.new_held = d_new_held, a.new_table = d_new_page_table, a.new_stride = new_pt_stride;
   a.new_refs = d_new_refs, a.missing = d_short;
   a.n_states = n_states;
+  a.copies = at<CopyList>(c->ws, c->wsm.fork_copies);
   launch_fork(a, (hipStream_t)stream);
   HIP_TRY(hipGetLastError());
   return DINFER_OK;

@@ -1,4 +1,6 @@
 // Operators of a search over several continuations (search.hpp).
+#include <type_traits>
+
 #include "cache.hpp"
 #include "search.hpp"
 
@@ -111,7 +113,7 @@ struct Candidate {
 __device__ inline bool better(const Candidate& x, const Candidate& y) { return x.score > y.score || (x.score == y.score && x.at < y.at); }
 
 constexpr int JOIN_THREADS = 1024, JOIN_WAVES = JOIN_THREADS / WAVE;
-constexpr int JOIN_CHUNKS = 1024, JOIN_LIST = 2048;                    // chunks that are read again, candidates that are ranked together
+constexpr int JOIN_CHUNKS = 1024, JOIN_LIST = 2048, JOIN_FEW = 256;    // chunks that are read again, candidates that are ranked together, and without another look
 constexpr int JOIN_ROWS = 4;                                           // rows of a wave whose chunks are under way together
 template <typename E>
 __global__ __launch_bounds__(JOIN_THREADS) void select_join_kernel(SelectArgs a, const ChunkState* state, int chunks) {
@@ -134,8 +136,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void select_join_kernel(SelectArgs a,
     if (!(p > -INFINITY) || !(m > -INFINITY)) return -INFINITY;
     return p < INFINITY ? (float)(n + (double)m) : m == INFINITY ? (float)n : -INFINITY;
   };
-  // A batch of rows: maximum and sum of each (a wave has JOIN_ROWS of them), the normalisers a lane per row, then the chunks' best.
-  float top = -INFINITY;
+  // A batch of rows: maximum and sum of each (a wave has JOIN_ROWS of them), the normalisers a lane per row.
   for (int b0 = 0; b0 < R; b0 += JOIN_WAVES * JOIN_ROWS) {
     const int r0 = b0 + wave;
     float M[JOIN_ROWS], s[JOIN_ROWS];
@@ -181,15 +182,12 @@ __global__ __launch_bounds__(JOIN_THREADS) void select_join_kernel(SelectArgs a,
       norm[mine] = held ? (double)base : some ? (double)base - ((p < INFINITY ? (double)p : 0.0) + log((double)row_sum[mine])) : 0.0;
     }
     __syncthreads();
-#pragma unroll
-    for (int u = 0; u < JOIN_ROWS; ++u) {
-      const int r = r0 + u * JOIN_WAVES;
-      if (r < R) top = fmaxf(top, head(norm[r], peak[r], M[u], lane == 0));
-    }
   }
-  // the K-th largest of the threads' best ones, or a little less: a bound from below by every wave's own, then among those that reach it
-  {
-    const uint32_t mine = order_of(top);
+  // The K-th largest of the threads' values, or a little less, NO_VALUE + 1 where fewer than K have one: a bound from below by every wave's own,
+  // then among those that reach it.
+  auto kth = [&](float value) {
+    const uint32_t mine = order_of(value);
+    if (threadIdx.x == 0) n_top = 0;
     uint32_t t = 0;
     for (int b = 31; b >= 16; --b) {
       const uint32_t up = t | 1u << b;
@@ -203,9 +201,9 @@ __global__ __launch_bounds__(JOIN_THREADS) void select_join_kernel(SelectArgs a,
     if (mine >= t && mine > NO_VALUE) tops[atomicAdd(&n_top, 1)] = mine;
     __syncthreads();
     if (wave == 0) {
-      constexpr int U = 4;
       const int n = n_top;
-      if (n >= K && n <= U * WAVE) {
+      auto search = [&](auto most) __attribute__((always_inline)) {
+        constexpr int U = decltype(most)::value;
         uint32_t x[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) x[u] = u * WAVE + lane < n ? tops[u * WAVE + lane] : 0;
@@ -217,12 +215,27 @@ __global__ __launch_bounds__(JOIN_THREADS) void select_join_kernel(SelectArgs a,
           for (int u = 0; u < U; ++u) reached += __popcll(__builtin_amdgcn_ballot_w64(x[u] >= up));
           if (reached >= K) t = up;
         }
-      }
-      if (lane == 0) least_of_all = max(t, NO_VALUE + 1);
+      };
+      if (n >= K && n <= 4 * WAVE) search(std::integral_constant<int, 4>{});
+      else if (n >= K) search(std::integral_constant<int, JOIN_WAVES>{});
+      if (lane == 0) least_of_all = n >= K ? max(t, NO_VALUE + 1) : NO_VALUE + 1;
     }
     __syncthreads();
+    return least_of_all;
+  };
+  const int units = R * chunks;
+  float top = -INFINITY;
+  for (int l0 = threadIdx.x; l0 < units; l0 += 4 * JOIN_THREADS) {
+    float m[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) m[u] = state[min(l0 + u * JOIN_THREADS, units - 1)].m;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int l = l0 + u * JOIN_THREADS;
+      if (l < units) top = fmaxf(top, head(norm[l / chunks], peak[l / chunks], m[u], l % chunks == 0));
+    }
   }
-  const uint32_t least = least_of_all;
+  uint32_t least = kth(top);
   // every chunk whose best candidate reaches it
   auto each_chunk = [&](auto use) {
     for (int r0 = wave; r0 < R; r0 += JOIN_WAVES * JOIN_ROWS)
@@ -253,13 +266,12 @@ __global__ __launch_bounds__(JOIN_THREADS) void select_join_kernel(SelectArgs a,
     a.token[out + k] = (int32_t)c.at;
     a.score_out[out + k] = (float)c.score;
   };
-  const double bound = (double)__uint_as_float(least & 0x80000000u ? least ^ 0x80000000u : ~least);
-  // the candidates of a chunk that reach it, in this wave
-  auto scan = [&](int r, int chunk, auto take) {
+  // The candidates of a chunk that reach it, in this wave: take(is one, candidate) in all lanes together.
+  auto scan = [&](int r, int chunk, auto take) __attribute__((always_inline)) {
     const float p = peak[r];
-    const double n = norm[r];
+    const double n = norm[r], bound = (double)__uint_as_float(least & 0x80000000u ? least ^ 0x80000000u : ~least);
     if (p != p) {
-      if (lane == 0) take(Candidate{n, (uint64_t)r << 32 | (uint32_t)a.hold[row0 + r]});
+      take(lane == 0, Candidate{n, (uint64_t)r << 32 | (uint32_t)a.hold[row0 + r]});
       return;
     }
     ChunkOf<E> x;
@@ -269,18 +281,39 @@ __global__ __launch_bounds__(JOIN_THREADS) void select_join_kernel(SelectArgs a,
 #pragma unroll
     for (int v = 0; v < CHUNK_VALUES; ++v) {
       const float z = x.value(v);
-      if (z >= cut && z > -INFINITY) {
+      const bool may = z >= cut && z > -INFINITY;
+      if (__builtin_amdgcn_ballot_w64(may)) {
         const double score = p < INFINITY ? n + (double)z : n;
-        if (order_of((float)score) >= least) take(Candidate{score, (uint64_t)r << 32 | (uint32_t)ChunkOf<E>::token(chunk, lane, v)});
+        take(may && order_of((float)score) >= least, Candidate{score, (uint64_t)r << 32 | (uint32_t)ChunkOf<E>::token(chunk, lane, v)});
       }
     }
   };
+  // Candidates into the list.  Where fewer than K chunks have one (turn 0), and where the list gets long, as the best rows' do that have many better
+  // than others' best (turn 2), the bound is first raised to that of the lanes' best ones in the listed chunks.  (If fewer than K lanes have
+  // one, all candidates together are no more than 32 * K.)
   if (n_chunks <= JOIN_CHUNKS) {
-    for (int i = wave; i < n_chunks; i += JOIN_WAVES)
-      scan(__builtin_amdgcn_readfirstlane(chunk_row[i]), __builtin_amdgcn_readfirstlane(chunk_at[i]), [&](const Candidate& c) {
-        const int at = atomicAdd(&n_list, 1);
-        if (at < JOIN_LIST) list[at] = c;
-      });
+    for (int turn = least == NO_VALUE + 1 ? 0 : 1; turn < 4; ++turn) {
+      const bool raise = turn % 2 == 0;
+      float best = -INFINITY;
+      for (int i = wave; i < n_chunks; i += JOIN_WAVES)
+        scan(__builtin_amdgcn_readfirstlane(chunk_row[i]), __builtin_amdgcn_readfirstlane(chunk_at[i]), [&](bool is, const Candidate& c) __attribute__((always_inline)) {
+          best = is ? fmaxf(best, (float)c.score) : best;
+          const uint64_t all = __builtin_amdgcn_ballot_w64(is);
+          if (raise || all == 0) return;
+          int at = 0;
+          if (lane == 0) at = atomicAdd(&n_list, (int)__popcll(all));
+          at = __builtin_amdgcn_readfirstlane(at) + __popcll(all & (lane ? ~0ull >> (64 - lane) : 0ull));
+          if (is && at < JOIN_LIST) list[at] = c;
+        });
+      if (raise) {
+        least = kth(best);
+        continue;
+      }
+      __syncthreads();
+      if (turn == 3 || n_list <= JOIN_FEW) break;
+      __syncthreads();      // (all have looked)
+      if (threadIdx.x == 0) n_list = 0;
+    }
   }
   __syncthreads();
   const int n = n_list;
@@ -308,8 +341,8 @@ __global__ __launch_bounds__(JOIN_THREADS) void select_join_kernel(SelectArgs a,
       Candidate mine{-INFINITY, ~0ull};
       each_chunk([&](int r, int c0, bool reaches) {
         for (uint64_t left = __builtin_amdgcn_ballot_w64(reaches); left; left &= left - 1)
-          scan(r, c0 + __builtin_ctzll(left), [&](const Candidate& c) {
-            if ((!begun || better(last, c)) && better(c, mine)) mine = c;
+          scan(r, c0 + __builtin_ctzll(left), [&](bool is, const Candidate& c) __attribute__((always_inline)) {
+            if (is && (!begun || better(last, c)) && better(c, mine)) mine = c;
           });
       });
 #pragma unroll
@@ -356,21 +389,28 @@ struct PageBits {
   uint64_t* word;
   int32_t* before;            // [words + 1]
   int words;
-  // Bits of the pages that `in` says yes to (every thread of the workgroup calls; ends with a barrier).
-  template <class In> __device__ void build(int n_pages, char* lds, In in) {
+  static constexpr int U = 8;
+  int first[U];               // counts of this thread's first pages: asked for early, and kept
+  __device__ static int page_of(int u) { return u * POOL_THREADS + threadIdx.x; }
+  __device__ void load(const int32_t* refs, int n_pages) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) first[u] = refs[min(page_of(u), n_pages - 1)];
+  }
+  // Bits of the pages whose count is (not) positive (every thread of the workgroup calls; ends with a barrier).
+  template <bool Used> __device__ void build(const int32_t* refs, int n_pages, char* lds) {
     words = (n_pages + 63) / 64;
     word = reinterpret_cast<uint64_t*>(lds);
     before = reinterpret_cast<int32_t*>(lds + (size_t)words * 8);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    constexpr int U = 8;
-    for (int w0 = wave * U; w0 < words; w0 += POOL_WAVES * U) {
-      bool is[U];
+    for (int w0 = wave; w0 < words; w0 += POOL_WAVES * U) {
+      int n[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) is[u] = in(min((w0 + u) * 64 + lane, n_pages - 1));
+      for (int u = 0; u < U; ++u) n[u] = w0 == wave ? first[u] : refs[min((w0 + u * POOL_WAVES) * 64 + lane, n_pages - 1)];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const uint64_t b = __builtin_amdgcn_ballot_w64(is[u] && (w0 + u) * 64 + lane < n_pages);
-        if (lane == 0 && w0 + u < words) word[w0 + u] = b;
+        const int w = w0 + u * POOL_WAVES;
+        const uint64_t b = __builtin_amdgcn_ballot_w64((n[u] > 0) == Used && w * 64 + lane < n_pages);
+        if (lane == 0 && w < words) word[w] = b;
       }
     }
     __shared__ int sums[POOL_WAVES];
@@ -447,10 +487,14 @@ struct Fork {
 __device__ inline Fork fork_of(const ForkArgs& a, int i) {      // i: the same in a whole wave
   const int all = a.parent[min((int)threadIdx.x & 63, a.n_new - 1)];
   Fork f;
-  f.parent = a.parent[i];
+  f.parent = __builtin_amdgcn_readlane(all, i);
   if (f.parent < 0 || f.parent >= a.n_old) f.parent = -1;
-  f.len = f.parent < 0 ? 0 : max(0, min(a.len[f.parent], a.limit));
-  f.held = f.parent < 0 ? 0 : max(0, min(a.held[f.parent], a.pt_stride));
+  f.len = f.held = 0;
+  if (a.n_old > 0) {
+    const int p = max(f.parent, 0), n = a.len[p], h = a.held[p];      // (no branch on the parent: several sequences' loads go together)
+    f.len = f.parent < 0 ? 0 : max(0, min(n, a.limit));
+    f.held = f.parent < 0 ? 0 : max(0, min(h, a.pt_stride));
+  }
   f.own = max(0, f.len - a.rewrite) / PAGE;
   f.have = (f.len + PAGE - 1) / PAGE;
   f.need = (int)min(((int64_t)f.len + a.room + PAGE - 1) / PAGE, (int64_t)a.new_stride);
@@ -462,55 +506,77 @@ __device__ inline int old_page(const ForkArgs& a, const Fork& f, int c) {      /
   return page >= 0 && page < a.pool.n_pages ? page : -1;
 }
 
-// The first launch, one workgroup: who gets which free page, the lowest ones in the order of sequences and columns.
+// The first launch, one workgroup: who gets which free page, the lowest ones in the order of sequences and columns, and the list of the
+// pages to copy.  A wave takes every POOL_WAVES-th sequence; what it finds out about the first 64 columns of their own it keeps.  Bound by its
+// chain of loads (parents, lengths, pages, counts) and, in pools of many pages, by one workgroup's reads of the counts.
+constexpr int FORK_SEQS = MAX_SEQS / POOL_WAVES;
 __global__ __launch_bounds__(POOL_THREADS) void fork_plan_kernel(ForkArgs a) {
   extern __shared__ __align__(16) char lds[];
-  __shared__ int wanted[MAX_SEQS];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  PageBits free;
-  free.build(a.pool.n_pages, lds, [&](int page) { return a.refs[page] <= 0; });
-  auto fresh_at = [&](const Fork& f, int c) {
-    if (c >= f.need) return false;
-    const int page = f.first ? old_page(a, f, c) : -1;
-    return page < 0 || a.refs[page] != 1;
+  __shared__ int wanted[MAX_SEQS], n_copies;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (threadIdx.x == 0) n_copies = 0;
+  auto look = [&](const Fork& f, int c, int& page) {      // does column c need another page than the parent's `page`
+    page = c < f.need ? old_page(a, f, c) : -1;
+    return c < f.need && !(f.first && page >= 0 && a.refs[max(page, 0)] == 1);
   };
-  for (int i = wave; i < a.n_new; i += POOL_WAVES) {
-    const Fork f = fork_of(a, i);
-    int n = 0;
-    for (int c0 = f.own; c0 < f.need; c0 += WAVE) n += __popcll(__builtin_amdgcn_ballot_w64(fresh_at(f, c0 + lane)));
-    if (lane == 0) wanted[i] = n;
+  PageBits free;
+  free.load(a.refs, a.pool.n_pages);
+  Fork f[FORK_SEQS];
+  int page[FORK_SEQS];
+  uint64_t fresh[FORK_SEQS];
+#pragma unroll
+  for (int u = 0; u < FORK_SEQS; ++u) f[u] = fork_of(a, min(wave + u * POOL_WAVES, a.n_new - 1));
+#pragma unroll
+  for (int u = 0; u < FORK_SEQS; ++u) fresh[u] = __builtin_amdgcn_ballot_w64(look(f[u], f[u].own + lane, page[u]));
+#pragma unroll
+  for (int u = 0; u < FORK_SEQS; ++u) {
+    int n = __popcll(fresh[u]), other;
+    for (int c0 = f[u].own + WAVE; c0 < f[u].need; c0 += WAVE) n += __popcll(__builtin_amdgcn_ballot_w64(look(f[u], c0 + lane, other)));
+    if (lane == 0 && wave + u * POOL_WAVES < a.n_new) wanted[wave + u * POOL_WAVES] = n;
   }
-  __syncthreads();
+  free.build<false>(a.refs, a.pool.n_pages, lds);
   const int upto = lane_scan(lane < a.n_new ? wanted[lane] : 0);      // (n_new <= 64)
   const int missing = max(0, __builtin_amdgcn_readlane(upto, 63) - free.total());
-  if (threadIdx.x == 0) *a.missing = missing;
+  if (threadIdx.x == 0) {
+    *a.missing = missing;
+    if (missing > 0) a.copies->n = 0;
+  }
   if (missing > 0) return;
   const uint64_t below = lane ? ~0ull >> (64 - lane) : 0ull;
-  for (int i = wave; i < a.n_new; i += POOL_WAVES) {
-    const Fork f = fork_of(a, i);
+#pragma unroll
+  for (int u = 0; u < FORK_SEQS; ++u) {
+    const int i = wave + u * POOL_WAVES;
+    if (i >= a.n_new) break;
     int at = __builtin_amdgcn_readlane(upto, i) - wanted[i];
     int32_t* row = a.new_table + (int64_t)i * a.new_stride;
-    for (int c0 = f.own; c0 < f.need; c0 += WAVE) {
+    for (int c0 = f[u].own; c0 < f[u].need; c0 += WAVE) {
       const int c = c0 + lane;
-      const bool fresh = fresh_at(f, c);
-      const uint64_t all = __builtin_amdgcn_ballot_w64(fresh);
-      if (fresh) row[c] = free.find<true>(at + __popcll(all & below));
-      else if (c < f.need) row[c] = old_page(a, f, c);
-      at += __popcll(all);
+      if (c0 > f[u].own) fresh[u] = __builtin_amdgcn_ballot_w64(look(f[u], c, page[u]));
+      if (fresh[u] >> lane & 1) {
+        const int to = free.find<true>(at + __popcll(fresh[u] & below));
+        row[c] = to;
+        if (c < f[u].have && page[u] >= 0) a.copies->page[atomicAdd(&n_copies, 1)] = int2{page[u], to};
+      } else if (c < f[u].need) row[c] = page[u];
+      at += __popcll(fresh[u]);
     }
     if (lane == 0) {
-      a.new_len[i] = f.len;
-      a.new_held[i] = f.need;
+      a.new_len[i] = f[u].len;
+      a.new_held[i] = f[u].need;
     }
   }
-  for (int p = threadIdx.x; p < a.pool.n_pages; p += POOL_THREADS) a.new_refs[p] = a.refs[p];
+#pragma unroll
+  for (int u = 0; u < PageBits::U; ++u)
+    if (PageBits::page_of(u) < a.pool.n_pages) a.new_refs[PageBits::page_of(u)] = free.first[u];
+  for (int p = PageBits::U * POOL_THREADS + threadIdx.x; p < a.pool.n_pages; p += POOL_THREADS) a.new_refs[p] = a.refs[p];
+  __syncthreads();
+  if (threadIdx.x == 0) a.copies->n = n_copies;
 }
 
 // The second: shared columns and the counts of all pages, the sequences' states, and the pages that are copied.
 struct ForkGrid {
   int state0, page0;          // first workgroups of the states and of the pages (in front: a row of the tables each)
   int state_pieces[MAX_STATES];
-  int columns, pieces;
+  int pieces;
 };
 __global__ __launch_bounds__(PIECE_THREADS) void fork_apply_kernel(ForkArgs a, ForkGrid g) {
   if (*a.missing > 0) return;
@@ -551,15 +617,18 @@ __global__ __launch_bounds__(PIECE_THREADS) void fork_apply_kernel(ForkArgs a, F
     return;
   }
   b -= g.page0;
-  const int piece = b % g.pieces, layer = b / g.pieces % a.pool.n_layers;
-  b /= g.pieces * a.pool.n_layers;
-  const Fork f = fork_of(a, b / g.columns);
-  const int c = f.own + b % g.columns;
-  if (c >= min(f.have, f.need)) return;
-  const int from = old_page(a, f, c), to = a.new_table[(int64_t)(b / g.columns) * a.new_stride + c];
-  if (from >= 0 && from != to) move_page_piece(a.pool, from, to, layer, piece);
+  const int piece = b % g.pieces, layer = b / g.pieces % a.pool.n_layers, copy = b / (g.pieces * a.pool.n_layers);
+  const int n = a.copies->n;
+  const int2 p = a.copies->page[copy];      // (as many as the launch has; beyond n: anything)
+  if (copy < n) move_page_piece(a.pool, p.x, p.y, layer, piece);
 }
 
+// Columns of a sequence that hold something and are written: from (len - rewrite) / PAGE on.
+static int fork_columns(int rewrite, int stride) {
+  const int n = (rewrite + PAGE - 1) / PAGE + 1;
+  return n < stride ? n : stride;
+}
+size_t fork_copies_bytes(int max_seqs, int max_pos) { return sizeof(CopyList) + (size_t)max_seqs * fork_columns(max_pos, INT32_MAX) * sizeof(int2); }
 void launch_fork(const ForkArgs& a, hipStream_t st) {
   ForkGrid g{};
   g.state0 = a.n_new + a.n_old;
@@ -568,11 +637,10 @@ void launch_fork(const ForkArgs& a, hipStream_t st) {
     g.state_pieces[k] = (int)((a.state[k].row_bytes + PIECE - 1) / PIECE);
     g.page0 += g.state_pieces[k] * a.n_new;
   }
-  g.columns = (a.rewrite + PAGE - 1) / PAGE + 1;      // that hold something and are written: from (len - rewrite) / PAGE on
-  if (g.columns > a.new_stride) g.columns = a.new_stride;
+  const int columns = fork_columns(a.rewrite, a.new_stride);
   g.pieces = page_pieces(a.pool);
   fork_plan_kernel<<<1, POOL_THREADS, page_bits_bytes(a.pool.n_pages), st>>>(a);
-  fork_apply_kernel<<<g.page0 + a.n_new * g.columns * a.pool.n_layers * g.pieces, PIECE_THREADS, 0, st>>>(a, g);
+  fork_apply_kernel<<<g.page0 + a.n_new * columns * a.pool.n_layers * g.pieces, PIECE_THREADS, 0, st>>>(a, g);
 }
 
 // ---------------------------------------------------------------- compact
@@ -581,13 +649,14 @@ __global__ __launch_bounds__(POOL_THREADS) void compact_plan_kernel(CompactArgs 
   extern __shared__ __align__(16) char lds[];
   const int n = a.pool.n_pages;
   PageBits used;
-  used.build(n, lds, [&](int page) { return a.refs[page] > 0; });
+  used.load(a.refs, n);
+  used.build<true>(a.refs, n, lds);
   const int front = used.total(), stay = front < n ? used.in_front(front) : front, moves = front - stay;
   if (threadIdx.x == 0) {
     a.count[0] = front;
     a.count[1] = moves;
   }
-  for (int p = threadIdx.x; p < n; p += POOL_THREADS) {
+  auto settle = [&](int p, int refs) {
     int to = -1;
     if (used.has(p)) {
       to = p;
@@ -596,12 +665,16 @@ __global__ __launch_bounds__(POOL_THREADS) void compact_plan_kernel(CompactArgs 
         to = used.find<false>(k);
         a.moved[n + k] = p;
       }
-      a.new_refs[to] = a.refs[p];
+      a.new_refs[to] = refs;
     }
     a.moved[p] = to;
     if (p >= front) a.new_refs[p] = 0;
     if (p >= moves) a.moved[n + p] = -1;
-  }
+  };
+#pragma unroll
+  for (int u = 0; u < PageBits::U; ++u)
+    if (PageBits::page_of(u) < n) settle(PageBits::page_of(u), used.first[u]);
+  for (int p = PageBits::U * POOL_THREADS + threadIdx.x; p < n; p += POOL_THREADS) settle(p, a.refs[p]);
 }
 __global__ __launch_bounds__(PIECE_THREADS) void compact_move_kernel(CompactArgs a, int pieces) {
   if ((int)blockIdx.x < a.n_seq) {

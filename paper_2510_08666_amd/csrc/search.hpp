@@ -34,6 +34,12 @@ struct StateRows {
   char* out;
   int64_t row_bytes;
 };
+// Pages to copy, left by a fork's first launch for its second.
+struct CopyList {
+  int32_t n, pad[3];
+  int2 page[1];               // from, to; n of them
+};
+size_t fork_copies_bytes(int max_seqs, int max_pos);
 struct ForkArgs {
   PagePool pool;
   int32_t n_old, n_new;
@@ -47,6 +53,7 @@ struct ForkArgs {
   int32_t *new_refs, *missing;
   StateRows state[MAX_STATES];
   int32_t n_states;
+  CopyList* copies;           // fork_copies_bytes
 };
 void launch_fork(const ForkArgs& a, hipStream_t st);
 

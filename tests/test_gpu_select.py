@@ -166,3 +166,14 @@ def test_refusals(m):
     with pytest.raises(b.DinferError):
         b.beam_select(z, score, row, row, out, scratch)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("ns,R,V,live,keep", [(4, 1, 4096, 1, 32), (2, 64, 9000, 3, 64), (1, 512, 1500, 512, 32), (3, 1, 100, 1, 64), (2, 40, 10, 40, 64), (1, 130, 2100, 70, 64)])
+def test_few_chunks_with_candidates(m, ns, R, V, live, keep):
+    """Fewer than n_keep stretches of logits that hold a candidate, many of them in each; many short rows."""
+    b, ops = m
+    g = torch.Generator().manual_seed(V)
+    z, score = 3 * torch.randn(ns, R, V, generator=g), -torch.rand(ns, R, generator=g)
+    for s in range(ns):
+        score[s, torch.randperm(R, generator=g)[live:]] = -math.inf
+    check(run(b, z.to(DEV), score.to(DEV), keep), ops.select(z, score, keep), keep)
