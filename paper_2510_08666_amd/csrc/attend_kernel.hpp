@@ -519,10 +519,15 @@ __global__ __launch_bounds__(ATTEND_WAVES * WAVE, (attend_waves_per_simd<E, HD>(
     float p[1][16];
     take_scores<DT, 1>(s, rule.factor(c2), m_run, l_run, o, p);
     if constexpr (PV) {
-      constexpr int PP = PvWeights<E>::PLANES;
+      // (two row tiles under a rule, where the matrix instructions count: one number per weight, rounded to nearest)
+      constexpr bool ONE = Rule::RANGES && RG == 2 && sizeof(E) == 2;
+      constexpr int PP = ONE ? 1 : PvWeights<E>::PLANES;
       vec pv[STEPS][PP];
 #pragma unroll
-      for (int s2 = 0; s2 < STEPS; ++s2) PvWeights<E>::split(p[0], s2, pv[s2]);
+      for (int s2 = 0; s2 < STEPS; ++s2) {
+        if constexpr (ONE) pv[s2][0] = PvStep<E>::p_vec(p[0], s2, 0);
+        else PvWeights<E>::split(p[0], s2, pv[s2]);
+      }
       if (decltype(tail)::value && odd) {
         // 0 * NaN would reach the rows that do not see the key: the product takes 0 in such a value's place, and the rows with
         // weight on it are found by products with its indicator, one kind (NaN, +inf, -inf) at a time, and marked

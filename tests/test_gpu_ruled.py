@@ -289,3 +289,23 @@ def test_the_form_of_many_rows(m, dtype, nh, hd, G, lens, past, rule_name):
                 assert abs(float(lse[t0 + i, h]) - norm) <= e + 2.0 ** -21 * abs(norm)
         t0 += n
     c.close()
+
+
+@pytest.mark.parametrize("lens,past", [([3, 40], [500, 0]), ([1300], [700])])
+def test_pages_beyond_32_bits(m, lens, past):
+    """The same rows in pages whose elements are numbered from 2^32 on (a pool of 8 GiB and more): the same bits, in both forms."""
+    from paper_2510_08666_amd import binding
+    cache, ops = m
+    c = cache.Cache("bf16", 16, 128, lens, past, seed=3)
+    first = 2 ** 32 // (2 * 16 * 128 * 16)      # elements of a page
+    far = binding.Context(c.cfg, first + c.n_pages, c.ns, 64, c.max_pos)
+    far.kv.view(torch.bfloat16).view(first + c.n_pages, -1)[first:].copy_(c.pool.view(c.n_pages, -1))
+    far.kv.view(torch.bfloat16).view(first + c.n_pages, -1)[:c.n_pages].zero_()
+    q = c.randn(c.T, 2048)
+    outs = [torch.zeros(c.T, 2048, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    for ctx, table, out in ((c.ctx, c.d_table, outs[0]), (far, torch.where(c.d_table >= 0, c.d_table + first, c.d_table), outs[1])):
+        ctx.attend_ruled(0, c.lens, c.d_past, table, q, out, block=1)
+    torch.cuda.synchronize()
+    assert torch.equal(*outs) and outs[0].abs().max() > 0
+    far.close()
+    c.close()
