@@ -448,7 +448,7 @@ int dinfer_attend_ruled(dinfer_ctx* ctx, int32_t layer, int32_t n_seq, const int
  * of row r scores  d_score[r] + z[r][v] - log(sum over u of exp(z[r][u])).  Needs no context; works on the current GPU.
  *   d_logits  n_seq * n_rows rows of `vocab` elements of `dtype` (DINFER_F32, DINFER_BF16), row_stride elements apart.  -infinity and NaN:
  *             no candidate, no weight.  If there are +infinities in a row, they share its weight.
- *   d_score   [n_seq][n_rows] float32; -infinity (or NaN): the row takes no part and is not read.
+ *   d_score   [n_seq][n_rows] float32; -infinity (or another value that is not finite): the row takes no part and is not read.
  *   d_hold    [n_seq][n_rows] or null: >= 0: the hypothesis is finished, its only candidate is this token, at d_score[r].
  *   d_row, d_token [n_seq][n_keep] out: the candidates, best first; equal scores: the lower row, then the lower token.  Where there are
  *             fewer: -1 (d_score_out -infinity).

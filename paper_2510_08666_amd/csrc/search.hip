@@ -38,9 +38,15 @@ template <typename E> struct ChunkOf {
     for (int n = 0; n < N; ++n) {
       const int at = token(chunk, lane, n * G);
       if (at + G <= vocab) __builtin_memcpy(&v[n], z + at, sizeof(v[n]));
-      else
+      else {
 #pragma unroll
-        for (int i = 0; i < G; ++i) v[n][i] = at + i < vocab ? z[at + i] : from_f32<E>(-INFINITY);
+        for (int i = 0; i < G; ++i) v[n][i] = from_f32<E>(-INFINITY);
+        if (at < vocab) {      // (one lane, where the row ends)
+#pragma unroll
+          for (int i = 0; i < G - 1; ++i)
+            if (at + i < vocab) v[n][i] = z[at + i];
+        }
+      }
     }
   }
   __device__ float raw(int r) const { return to_f32(v[r / G][r % G]); }
@@ -76,7 +82,7 @@ template <typename E, int PER>
 __global__ __launch_bounds__(SELECT_THREADS) void select_chunk_kernel(SelectArgs a, ChunkState* state, int chunks) {
   const int64_t row = blockIdx.y;
   const int chunk0 = (blockIdx.x * SELECT_WAVES + (threadIdx.x >> 6)) * PER, lane = threadIdx.x & 63;
-  if (chunk0 >= chunks || !(a.score[row] > -INFINITY) || (a.hold && a.hold[row] >= 0)) return;
+  if (chunk0 >= chunks || !(fabsf(a.score[row]) < INFINITY) || (a.hold && a.hold[row] >= 0)) return;
   const E* z = (const E*)a.logits + row * a.row_stride;
   ChunkOf<E> x, next;
   x.load(z, a.vocab, chunk0, lane);
@@ -113,7 +119,7 @@ struct Candidate {
 __device__ inline bool better(const Candidate& x, const Candidate& y) { return x.score > y.score || (x.score == y.score && x.at < y.at); }
 
 constexpr int JOIN_THREADS = 1024, JOIN_WAVES = JOIN_THREADS / WAVE;
-constexpr int JOIN_CHUNKS = 1024, JOIN_LIST = 2048, JOIN_FEW = 256;    // chunks that are read again, candidates that are ranked together, and without another look
+constexpr int JOIN_CHUNKS = 1024, JOIN_LIST = 2048, JOIN_FEW = 256, JOIN_ALL = 64;    // chunks that are read again, candidates that are ranked together, and without another look
 constexpr int JOIN_ROWS = 4;                                           // rows of a wave whose chunks are under way together
 template <typename E>
 __global__ __launch_bounds__(JOIN_THREADS) void select_join_kernel(SelectArgs a, const ChunkState* state, int chunks) {
@@ -176,7 +182,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void select_join_kernel(SelectArgs a,
     __syncthreads();
     if (threadIdx.x < JOIN_WAVES * JOIN_ROWS && b0 + (int)threadIdx.x < R) {
       const float p = peak[mine];
-      const bool live = base > -INFINITY, held = live && a.hold && hold >= 0, some = live && !held && p > -INFINITY;
+      const bool live = fabsf(base) < INFINITY, held = live && a.hold && hold >= 0, some = live && !held && p > -INFINITY;
       peak[mine] = held ? __builtin_nanf("") : some ? p : -INFINITY;
       // (infinite logits share the row's weight: log(1 / their number) each)
       norm[mine] = held ? (double)base : some ? (double)base - ((p < INFINITY ? (double)p : 0.0) + log((double)row_sum[mine])) : 0.0;
@@ -223,9 +229,10 @@ __global__ __launch_bounds__(JOIN_THREADS) void select_join_kernel(SelectArgs a,
     __syncthreads();
     return least_of_all;
   };
+  // (of 64 chunks or less all are read again: the bound comes from what is in them, below)
   const int units = R * chunks;
   float top = -INFINITY;
-  for (int l0 = threadIdx.x; l0 < units; l0 += 4 * JOIN_THREADS) {
+  for (int l0 = threadIdx.x; l0 < units && units > JOIN_ALL; l0 += 4 * JOIN_THREADS) {
     float m[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) m[u] = state[min(l0 + u * JOIN_THREADS, units - 1)].m;
@@ -235,7 +242,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void select_join_kernel(SelectArgs a,
       if (l < units) top = fmaxf(top, head(norm[l / chunks], peak[l / chunks], m[u], l % chunks == 0));
     }
   }
-  uint32_t least = kth(top);
+  uint32_t least = units > JOIN_ALL ? kth(top) : NO_VALUE + 1;
   // every chunk whose best candidate reaches it
   auto each_chunk = [&](auto use) {
     for (int r0 = wave; r0 < R; r0 += JOIN_WAVES * JOIN_ROWS)
@@ -267,15 +274,16 @@ __global__ __launch_bounds__(JOIN_THREADS) void select_join_kernel(SelectArgs a,
     a.score_out[out + k] = (float)c.score;
   };
   // The candidates of a chunk that reach it, in this wave: take(is one, candidate) in all lanes together.
-  auto scan = [&](int r, int chunk, auto take) __attribute__((always_inline)) {
+  auto load = [&](int r, int chunk, ChunkOf<E>& x) __attribute__((always_inline)) {
+    x.load((const E*)a.logits + (row0 + r) * a.row_stride, peak[r] != peak[r] ? 0 : a.vocab, chunk, lane);
+  };
+  auto scan = [&](int r, int chunk, const ChunkOf<E>& x, auto take) __attribute__((always_inline)) {
     const float p = peak[r];
     const double n = norm[r], bound = (double)__uint_as_float(least & 0x80000000u ? least ^ 0x80000000u : ~least);
     if (p != p) {
       take(lane == 0, Candidate{n, (uint64_t)r << 32 | (uint32_t)a.hold[row0 + r]});
       return;
     }
-    ChunkOf<E> x;
-    x.load((const E*)a.logits + (row0 + r) * a.row_stride, a.vocab, chunk, lane);
     // (a logit below `cut` cannot; those above it are looked at)
     const float cut = p < INFINITY ? (float)(bound - n - (fabs(bound) + fabs(n) + 1.0) * 0x1p-20) : INFINITY;
 #pragma unroll
@@ -292,19 +300,31 @@ __global__ __launch_bounds__(JOIN_THREADS) void select_join_kernel(SelectArgs a,
   // than others' best (turn 2), the bound is first raised to that of the lanes' best ones in the listed chunks.  (If fewer than K lanes have
   // one, all candidates together are no more than 32 * K.)
   if (n_chunks <= JOIN_CHUNKS) {
+    ChunkOf<E> kept;      // a wave's first one
+    if (wave < n_chunks) load(__builtin_amdgcn_readfirstlane(chunk_row[wave]), __builtin_amdgcn_readfirstlane(chunk_at[wave]), kept);
     for (int turn = least == NO_VALUE + 1 ? 0 : 1; turn < 4; ++turn) {
       const bool raise = turn % 2 == 0;
       float best = -INFINITY;
-      for (int i = wave; i < n_chunks; i += JOIN_WAVES)
-        scan(__builtin_amdgcn_readfirstlane(chunk_row[i]), __builtin_amdgcn_readfirstlane(chunk_at[i]), [&](bool is, const Candidate& c) __attribute__((always_inline)) {
-          best = is ? fmaxf(best, (float)c.score) : best;
+      for (int i = wave; i < n_chunks; i += JOIN_WAVES) {
+        const int r = __builtin_amdgcn_readfirstlane(chunk_row[i]), chunk = __builtin_amdgcn_readfirstlane(chunk_at[i]);
+        ChunkOf<E> x = kept;
+        if (i != wave) load(r, chunk, x);
+        if (raise) {
+          float z = -INFINITY;
+#pragma unroll
+          for (int v = 0; v < CHUNK_VALUES; ++v) z = fmaxf(z, x.value(v));
+          best = fmaxf(best, head(norm[r], peak[r], z, lane == 0));      // (the larger logit, the better)
+          continue;
+        }
+        scan(r, chunk, x, [&](bool is, const Candidate& c) __attribute__((always_inline)) {
           const uint64_t all = __builtin_amdgcn_ballot_w64(is);
-          if (raise || all == 0) return;
+          if (all == 0) return;
           int at = 0;
           if (lane == 0) at = atomicAdd(&n_list, (int)__popcll(all));
           at = __builtin_amdgcn_readfirstlane(at) + __popcll(all & (lane ? ~0ull >> (64 - lane) : 0ull));
           if (is && at < JOIN_LIST) list[at] = c;
         });
+      }
       if (raise) {
         least = kth(best);
         continue;
@@ -340,10 +360,13 @@ __global__ __launch_bounds__(JOIN_THREADS) void select_join_kernel(SelectArgs a,
     for (filled = 0; filled < K; ++filled) {
       Candidate mine{-INFINITY, ~0ull};
       each_chunk([&](int r, int c0, bool reaches) {
-        for (uint64_t left = __builtin_amdgcn_ballot_w64(reaches); left; left &= left - 1)
-          scan(r, c0 + __builtin_ctzll(left), [&](bool is, const Candidate& c) __attribute__((always_inline)) {
+        for (uint64_t left = __builtin_amdgcn_ballot_w64(reaches); left; left &= left - 1) {
+          ChunkOf<E> x;
+          load(r, c0 + __builtin_ctzll(left), x);
+          scan(r, c0 + __builtin_ctzll(left), x, [&](bool is, const Candidate& c) __attribute__((always_inline)) {
             if (is && (!begun || better(last, c)) && better(c, mine)) mine = c;
           });
+        }
       });
 #pragma unroll
       for (int d = 32; d > 0; d >>= 1) {

@@ -14,7 +14,7 @@ struct SelectArgs {
   const void* logits;         // [n_seq * n_rows] rows of vocab, row_stride elements apart
   int64_t row_stride;
   int32_t n_seq, n_rows, vocab, n_keep;
-  const float* score;         // [n_seq][n_rows], -inf: the row takes no part
+  const float* score;         // [n_seq][n_rows], not finite: the row takes no part
   const int32_t* hold;        // [n_seq][n_rows] or null: >= 0: the row's only candidate
   int32_t *row, *token;       // [n_seq][n_keep]
   float* score_out;

@@ -88,7 +88,7 @@ def select(logits, score, keep, hold=None):
         found = []
         for r in range(logits.shape[1]):
             base = float(score[s, r])
-            if not base > -math.inf:
+            if not math.isfinite(base):
                 continue
             if hold is not None and int(hold[s, r]) >= 0:
                 found.append((base, r, int(hold[s, r])))

@@ -245,3 +245,25 @@ def test_refusals(m):
             pool.ctx.kv_compact(**{**good, **bad})
     torch.cuda.synchronize()
     pool.close()
+
+
+def test_pages_beyond_32_bits(m):
+    """Pages that lie beyond 4 GiB of a layer are shared, copied and packed as others are."""
+    _, b, _ = m
+    n = 2 ** 33 // (2 * 2 * 16 * 16 * 128) + 40      # pages of 128 KiB
+    pool = Pool(m, 2, dtype="bf16", heads=16, head_dim=128, layers=1)
+    pool.close()
+    di = m[0]
+    cfg = di.configs.scaled(di.model_preset("tiny"), n_layers=1, hidden=64, n_heads=16, head_dim=128, n_experts=1, top_k=1, moe_inter=64, vocab=64, dtype="bf16")
+    pool.ctx, pool.n = b.Context(cfg, n, 4, 64, 2048), n
+    kv = pool.ctx.kv.view(I32).view(n, -1)
+    kv[n - 9:].copy_(torch.randint(0, 2 ** 31 - 1, (9, kv.shape[1]), dtype=I32))
+    refs = [0] * (n - 10) + [0] + [1] * 9
+    got = pool.fork([0, 0], [20], [2], [[n - 3, n - 1]], [2] * (n - 10) + [0, 2, 2, 2, 2, 2, 2, 1, 2, 1], 5, 0, 3)
+    assert got["short"] == [0] and got["d_new_page_table"] == [[n - 3, n - 1, -1], [n - 3, n - 10, -1]]
+    assert torch.equal(kv[n - 10], kv[n - 1])
+    table, new_refs, moved, count = ints([[0, 0]]), ints([0] * n), torch.zeros(2, n, dtype=I32, device=DEV), ints([0, 0])
+    pool.ctx.kv_compact(ints([2]), ints([[n - 1, n - 9]]), ints(refs), table, new_refs, moved, count)
+    torch.cuda.synchronize()
+    assert count.tolist() == [9, 9] and table.tolist() == [[8, 0]] and torch.equal(kv[:9], kv[n - 9:])
+    pool.close()

@@ -105,6 +105,7 @@ def test_odd_values(m):
     ref = ops.select(z, score, 24)
     check(run(b, z.to(DEV), score.to(DEV), 24), ref, 24)
     dead = torch.full((1, 8), -math.inf, device=DEV)
+    dead[0, 1:4] = torch.tensor([math.inf, math.nan, math.inf])
     row, token, out = run(b, z.to(DEV), dead, 3)
     assert (row == -1).all() and (token == -1).all() and (out == -math.inf).all()
     hold = torch.full((1, 8), 4, dtype=I32, device=DEV)
