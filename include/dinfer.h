@@ -316,7 +316,8 @@ int dinfer_kv_read(dinfer_ctx* ctx, int32_t layer, const int32_t* d_page_row, in
  * belongs to cache head i / (n_q_heads / n_heads).  `layer` chooses the part of the pool.  The context must be used
  * with the GPU that was current at dinfer_create (DINFER_EINVAL otherwise).  Sums, statistics and angles are float32 or
  * wider; outputs are rounded once.  (Attention weights of a bfloat16 cache enter the product with the values as two bfloat16
- * numbers each, which are within 2^-15 of the weight together.) */
+ * numbers each, which are within 2^-15 of the weight together; in dinfer_attend_ruled, where a sequence has more than 32 rows, as one,
+ * within 2^-9.) */
 
 /* A rotation of the first rotary_dim features of a head (even, at most head_dim; the others pass through): pairs
  * (j, j + rotary_dim/2), or (2j, 2j+1) with interleaved != 0, turn by position * f_j, f_j = theta^(-2j/rotary_dim) changed by
@@ -454,7 +455,8 @@ int dinfer_attend_ruled(dinfer_ctx* ctx, int32_t layer, int32_t n_seq, const int
  *             fewer: -1 (d_score_out -infinity).
  *   d_score_out [n_seq][n_keep] out; may not be d_score.
  *   d_scratch 256-byte aligned, dinfer_beam_scratch_bytes (0: a size out of range), contents irrelevant.
- * Scores are compared in 64 bits and rounded once.  n_keep <= 64, n_rows <= 1024, n_seq * n_rows <= 65535, vocab <= 2^24. */
+ * Scores are compared in 64 bits and rounded once.  (Thousands of candidates with one and the same score at the border of the best n_keep
+ * take n_keep passes over them: right, but slow.)  n_keep <= 64, n_rows <= 1024, n_seq * n_rows <= 65535, vocab <= 2^24. */
 size_t dinfer_beam_scratch_bytes(int32_t n_seq, int32_t n_rows, int32_t vocab, int32_t n_keep);
 int dinfer_beam_select(const void* d_logits, int32_t dtype, int64_t row_stride, int32_t n_seq, int32_t n_rows, int32_t vocab,
                        const float* d_score, const int32_t* d_hold, int32_t n_keep, int32_t* d_row, int32_t* d_token,

@@ -2,6 +2,14 @@
 // prefix that all see, documents, capped scores, a bias by distance.  What a row sees is at most two ranges of cache positions
 // (row_ranges), so that a group of rows walks only the key tiles in which it sees anything, and looks at single keys only in
 // those that not all of them see whole.
+//
+// Bound: the matrix instructions of the pairs that are seen (4 * head_dim operations each, at the 1.23 PFLOP/s of a large matrix product) or, for
+// few rows, one read of the keys and values.  Few rows take the kernel of attend_kernel.hpp with RangeRule for its words: a token behind
+// 511 positions 10.2 us (the chain of dependent loads), 48 tokens behind 1000 to 8000 in a window of 4097 with 8 heads of 4 queries 135 us (4.9 TB/s),
+// 512 tokens behind 4096, causal by blocks of 32, 39.9 us (0.46 PFLOP/s), prompts of 333 to 1811 tokens in documents of 301 with capped scores
+// 59 us (0.17 PFLOP/s, most tiles partly seen).  Two row tiles hold their weights as one bfloat16 number (off by 2^-9 at most), which takes half
+// as many matrix instructions out of the product with the values: 47.0 -> 43.2 us and 63.6 -> 60.2 with the joins; one row tile waits for
+// memory and keeps two.
 #include "attend_kernel.hpp"
 
 namespace dinfer {
@@ -11,8 +19,11 @@ namespace dinfer {
 // weights, 32 matrix instructions that are fed from LDS without a pause), while the other one works out the exponentials of the scores that
 // it multiplied in the phase before, and brings its share of a later tile in; then they change places.  Four buffers: a wave of the half that is behind still reads
 // tile i while tile i + 3 comes in.  Weights enter the product with the values as one bfloat16 number each, rounded to nearest (off by
-// 2^-9 at most; the sum of a row is that of the weights before): a second one, as in the form of few rows, which waits for memory, would
-// be half as many matrix instructions more.
+// 2^-9 at most; the sum of a row is that of the weights before): a second one would be half as many matrix instructions more.
+// A causal prompt of 8191 tokens, 8 heads of 4 queries and 128 features: 544 us, 1.01 PFLOP/s.  A phase of matrix work takes 1480 cycles, 1024 of them
+// the instructions' own, LDS gives 119 bytes a cycle, and the clock is 1.88 GHz.  Slower were: 4 waves of 32 rows, the phases woven in one
+// wave, two workgroups per compute unit (620 to 640 us); 64 rows per wave (842 and more, accumulators move between register files);
+// half of the values straight from L1 (813).
 constexpr int RULED_WAVES = 8, RULED_BUFFERS = 4, KEYS = 2 * TILE, RULED_ROWS = RULED_WAVES * TILE;
 template <int HD> constexpr size_t ruled_rows_lds() { return (size_t)RULED_BUFFERS * 4 * (HD / ET<bf16_t>::KS) * WAVE * 16 + (ATTN_MAX_PAGES + 4) * 4; }
 // (NaN if one of them is: a row with such a score is not a number anyway, and the instruction takes matrix results as they are)
@@ -294,12 +305,12 @@ static int64_t likely_meetings(const AttendArgs& a) {
   return sum * a.geom.n_heads / (a.rule.first || a.rule.end ? 4 : 1);      // (documents: most of them are much shorter than the sequence)
 }
 // The form of many rows where a call has that many of them (counted in heads of 128 features).  Its workgroups are few and take 10 us to begin
-// and end; against two row tiles per workgroup, 16 heads unless stated, in us: a causal prompt of 1000 tokens (8 thousand meetings) 47.8 and
-// 34.1, of 2000 (32) 65 and 62, of 4000 (126) 127 and 158; 256 tokens behind 4096 (17) 48 and 33, 1024 behind 4096 (74) 72 and 83, 2048 behind
-// 4096 (165) 123 and 164, 512 behind 12000 (98) 84 and 96; 8 heads of 4 queries: 512 behind 2000 (36) 51 and 50, 2000 causal (63) 69 and 82; 8000
-// tokens in a window of 512 (67) 104 and 101, of 2048 (259) 184 and 232; four prompts of 1811 in documents of 301 (52) 103 and 97; 4 heads of 2 queries
-// and 64 features, 4000 causal (62) 63 and 62.
-constexpr int64_t RULED_MEETINGS = 3 << 14;
+// and end; against two row tiles per workgroup, 16 heads unless stated, in us: a causal prompt of 1000 tokens (8 thousand meetings) 48 and
+// 33, of 2000 (32) 64 and 54, of 4000 (126) 125 and 143; 256 tokens behind 4096 (17) 48 and 32, 1024 behind 4096 (74) 73 and 74, 2048 behind
+// 4096 (165) 126 and 139, 512 behind 12000 (98) 84 and 85; 8 heads of 4 queries: 512 behind 2000 (36) 53 and 46, 2000 causal (63) 70 and 72; 8000
+// tokens in a window of 512 (67) 105 and 93, of 2048 (259) 189 and 210; four prompts of 1811 in documents of 301 (52) 106 and 94; 4 heads of 2 queries
+// and 64 features, 4000 causal (62) 64 and 57.
+constexpr int64_t RULED_MEETINGS = 5 << 14;
 template <class Rule, int HD> static void launch_ruled_t(bool bf16, const AttendArgs& a, hipStream_t st) {
   const int most = most_rows(a.tok.span, a.group);
   if (!bf16) launch_attend_t<float, HD, 1, 1, true, Rule>(a, st);

@@ -11,6 +11,9 @@ namespace dinfer {
 // once and leaves the maximum and the sum of exponentials of every chunk of 2048.  The second one, a workgroup per sequence, works
 // the rows' normalisers out of them, and a threshold: the n_keep-th best of the chunks' best candidates is no better than the n_keep-th
 // best candidate, so that only chunks that reach it, about n_keep of them, are read again, and what reaches it there is ranked, in 64 bits.
+// Bound: one read of the logits.  8 sequences of 64 rows of 157184 bfloat16, six rows of ten live (98 MB): the stream 19.7 us (5.0 TB/s), the join 17.0 (a chain of short
+// steps, 1024 threads: normalisers 4.5, the bound 2.4, the list of chunks 2.1, reading them 3.1, ranking 1.7); one launch that kept every
+// row's best ones as it went took 74.7.  4 rows of float32: 3.4 + 10.4.
 constexpr int CHUNK_VALUES = 32, CHUNK = WAVE * CHUNK_VALUES;          // logits of a lane, in registers, and of a wave
 constexpr int SELECT_THREADS = 256, SELECT_WAVES = SELECT_THREADS / WAVE;
 constexpr uint32_t NO_VALUE = 0x007fffffu;                             // order_of(-inf): no candidate
@@ -531,7 +534,8 @@ __device__ inline int old_page(const ForkArgs& a, const Fork& f, int c) {      /
 
 // The first launch, one workgroup: who gets which free page, the lowest ones in the order of sequences and columns, and the list of the
 // pages to copy.  A wave takes every POOL_WAVES-th sequence; what it finds out about the first 64 columns of their own it keeps.  Bound by its
-// chain of loads (parents, lengths, pages, counts) and, in pools of many pages, by one workgroup's reads of the counts.
+// chain of loads (parents, lengths, pages, counts) and, in pools of many pages, by one workgroup's reads of the counts.  4 sequences 5.4 us, 64 of them
+// behind up to 4001 positions 10.5.
 constexpr int FORK_SEQS = MAX_SEQS / POOL_WAVES;
 __global__ __launch_bounds__(POOL_THREADS) void fork_plan_kernel(ForkArgs a) {
   extern __shared__ __align__(16) char lds[];
@@ -595,7 +599,8 @@ __global__ __launch_bounds__(POOL_THREADS) void fork_plan_kernel(ForkArgs a) {
   if (threadIdx.x == 0) a.copies->n = n_copies;
 }
 
-// The second: shared columns and the counts of all pages, the sequences' states, and the pages that are copied.
+// The second: shared columns and the counts of all pages, the sequences' states, and the pages that are copied.  Bound by their bytes,
+// once each way: 64 sequences, 69 MB, 11.9 us.  (Workgroups that looked for themselves what to copy: 28.7 us both launches, with the list 25.0.)
 struct ForkGrid {
   int state0, page0;          // first workgroups of the states and of the pages (in front: a row of the tables each)
   int state_pieces[MAX_STATES];
@@ -667,7 +672,9 @@ void launch_fork(const ForkArgs& a, hipStream_t st) {
 }
 
 // ---------------------------------------------------------------- compact
-// The k-th page in use behind the front goes to the k-th free page in the front, the front being as long as there are pages in use.
+// The k-th page in use behind the front goes to the k-th free page in the front, the front being as long as there are pages in use, so that no
+// page is moved twice and none is overwritten that is still to be read.  Plan: bound by its loads in turn (3.0 us; 6.3 with 48 sequences; counts
+// that were read again for every use took 10.5).  Move: bound by its bytes, 131 us for 665 MB both ways, 5.08 TB/s, the rate of a copy.
 __global__ __launch_bounds__(POOL_THREADS) void compact_plan_kernel(CompactArgs a) {
   extern __shared__ __align__(16) char lds[];
   const int n = a.pool.n_pages;
