@@ -439,8 +439,9 @@ typedef struct {
 } dinfer_attend_rule;
 
 /* dinfer_attend with a rule in the place of visibility words, and any number of new tokens.  What lies in keys and values that a token
- * does not see, infinities and NaN included, does not reach it; a token that sees nothing gets zeros (d_lse -infinity).  The bound
- * on the size of a call is dinfer_attend's. */
+ * does not see, infinities and NaN included, does not reach it; a token that sees nothing gets zeros (d_lse -infinity).  A value that is
+ * not finite, seen with less than 2^-126 of the row's largest weight, which is 0 in float32, gives NaN or nothing.  The bound on the size
+ * of a call is dinfer_attend's. */
 int dinfer_attend_ruled(dinfer_ctx* ctx, int32_t layer, int32_t n_seq, const int32_t* h_lens, const int32_t* d_past,
                         const int32_t* d_page_table, int32_t pt_stride, const void* d_q, int64_t q_stride, int32_t n_q_heads,
                         const dinfer_attend_rule* rule, float scale, void* d_out, int64_t out_stride, float* d_lse, void* stream);

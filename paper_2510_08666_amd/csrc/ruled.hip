@@ -7,67 +7,77 @@
 // few rows, one read of the keys and values.  Few rows take the kernel of attend_kernel.hpp with RangeRule for its words: a token behind
 // 511 positions 10.2 us (the chain of dependent loads), 48 tokens behind 1000 to 8000 in a window of 4097 with 8 heads of 4 queries 135 us (4.9 TB/s),
 // 512 tokens behind 4096, causal by blocks of 32, 39.9 us (0.46 PFLOP/s), prompts of 333 to 1811 tokens in documents of 301 with capped scores
-// 59 us (0.17 PFLOP/s, most tiles partly seen).  Two row tiles hold their weights as one bfloat16 number (off by 2^-9 at most), which takes half
+// 59 us (0.17 PFLOP/s: groups of rows in two documents walk both, all tiles partly seen, and end last).  Two row tiles hold their weights as one bfloat16 number (off by 2^-9 at most), which takes half
 // as many matrix instructions out of the product with the values: 47.0 -> 43.2 us and 63.6 -> 60.2 with the joins; one row tile waits for
 // memory and keeps two.
 #include "attend_kernel.hpp"
 
 namespace dinfer {
 
-// Many rows: a workgroup takes 256 rows of a cache head, a wave 32 of them, and key tiles of 64 go through LDS once for all of them.  The
-// two waves of a SIMD take turns: in one phase a wave multiplies (the next tile's keys with its queries, this tile's values with their
-// weights, 32 matrix instructions that are fed from LDS without a pause), while the other one works out the exponentials of the scores that
-// it multiplied in the phase before, and brings its share of a later tile in; then they change places.  Four buffers: a wave of the half that is behind still reads
-// tile i while tile i + 3 comes in.  Weights enter the product with the values as one bfloat16 number each, rounded to nearest (off by
-// 2^-9 at most; the sum of a row is that of the weights before): a second one would be half as many matrix instructions more.
-// A causal prompt of 8191 tokens, 8 heads of 4 queries and 128 features: 544 us, 1.01 PFLOP/s.  A phase of matrix work takes 1480 cycles, 1024 of them
-// the instructions' own, LDS gives 119 bytes a cycle, and the clock is 1.88 GHz.  Slower were: 4 waves of 32 rows, the phases woven in one
-// wave, two workgroups per compute unit (620 to 640 us); 64 rows per wave (842 and more, accumulators move between register files);
-// half of the values straight from L1 (813).
-constexpr int RULED_WAVES = 8, RULED_BUFFERS = 4, KEYS = 2 * TILE, RULED_ROWS = RULED_WAVES * TILE;
-template <int HD> constexpr size_t ruled_rows_lds() { return (size_t)RULED_BUFFERS * 4 * (HD / ET<bf16_t>::KS) * WAVE * 16 + (ATTN_MAX_PAGES + 4) * 4; }
+// Many rows: a wave takes 32 rows of a cache head, a workgroup of WAVES waves WAVES times as many, and key tiles go through LDS once for
+// all of them.  In a turn a wave multiplies (the next tile's keys with its queries, this tile's values with their weights, matrix
+// instructions that are fed from LDS without a pause), brings in its share of a later tile and works out the exponentials of the scores that
+// it multiplied.  Four buffers: V of tile i, K of tile i + 1, the first fragments of K of tile i + 2, tile i + 3 on its way in.  Weights enter
+// the product with the values as one bfloat16 number each, rounded to nearest (off by 2^-9 at most; the sum of a row is that of the
+// weights before): a second one would be half as many matrix instructions more.
+//
+// WAVES = 4: 128 rows, tiles of 32 keys, two workgroups per compute unit, whose waves on a SIMD cover each other as they come; loads are under way
+// for two turns.  A workgroup alone on its compute unit takes 1800 cycles a turn, 512 of them its matrix instructions.
+// WAVES = 8: 256 rows, tiles of 64 keys, one workgroup per compute unit, and the two waves of a SIMD in two phases by barriers: one multiplies
+// while the other one does the rest, then they change places; a wave of the half that is behind still reads tile i while tile i + 3 comes in.
+// A causal prompt of 8191 tokens, 8 heads of 4 queries and 128 features: 544 us, 1.01 PFLOP/s (WAVES = 4: 595).  A phase of matrix work takes 1480
+// cycles, 1024 of them the instructions' own, LDS gives 119 bytes a cycle, and the clock is 1.88 GHz.  Slower were: 4 waves of 32 rows with
+// the products of two tiles woven together (620 to 640 us); 64 rows per wave (842 and more, accumulators move between register files); half of the
+// values straight from L1 (813).
+constexpr int RULED_BUFFERS = 4;
+constexpr int key_tiles(int waves) { return waves / 4; }      // of 32 keys, that go through LDS together
+template <int HD, int WAVES> constexpr size_t ruled_rows_lds() {
+  return (size_t)RULED_BUFFERS * 2 * key_tiles(WAVES) * (HD / ET<bf16_t>::KS) * WAVE * 16 + (ATTN_MAX_PAGES + 4) * 4;
+}
 // (NaN if one of them is: a row with such a score is not a number anyway, and the instruction takes matrix results as they are)
 __device__ inline float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 __device__ inline float both_halves_max(float v) {
   const auto w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return larger(__uint_as_float(w[0]), __uint_as_float(w[1]));
 }
-template <class Rule, int HD>
-__global__ __launch_bounds__(RULED_WAVES * WAVE, 2) void ruled_rows_kernel(AttendArgs a, const int32_t* __restrict__ live) {
+template <class Rule, int HD, int WAVES>
+__global__ __launch_bounds__(WAVES * WAVE, 2) void ruled_rows_kernel(AttendArgs a, const int32_t* __restrict__ live) {
   if (step_is_dead(live)) return;
   typedef bf16_t E;
   typedef ET<E>::vec vec;
-  constexpr int G = ET<E>::G, KS = ET<E>::KS, DSTEPS = HD / KS, DT = HD / TILE, STEPS = KEYS / PAGE;
+  constexpr int G = ET<E>::G, KS = ET<E>::KS, DSTEPS = HD / KS, DT = HD / TILE, NT = key_tiles(WAVES), KEYS = NT * TILE, STEPS = KEYS / PAGE, ROWS = WAVES * TILE;
+  constexpr bool PHASES = WAVES == 8;
+  constexpr int SETS = PHASES ? 1 : 2, AHEAD = 3 + SETS;      // tiles on their way in, and how far in front of its products a tile's loads are issued
   // Fragments of a tile, K and then V, and those that a wave fetches: of K consecutive steps of one row tile, of V feature tiles of one step.
-  constexpr int KF = 2 * DSTEPS, VF = STEPS * DT, FRAGS = KF + VF, K_MINE = KF / RULED_WAVES, V_MINE = VF / RULED_WAVES;
-  static_assert(K_MINE * RULED_WAVES == KF && V_MINE * RULED_WAVES == VF && DSTEPS % K_MINE == 0 && DT % V_MINE == 0, "whole fragments");
+  constexpr int KF = NT * DSTEPS, VF = STEPS * DT, FRAGS = KF + VF, K_MINE = KF / WAVES, V_MINE = VF / WAVES;
+  static_assert(K_MINE * WAVES == KF && V_MINE * WAVES == VF && DSTEPS % K_MINE == 0 && DT % V_MINE == 0, "whole fragments");
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
   const E* kv = (const E*)a.kv_layer;
   extern __shared__ __align__(16) char smem[];
   auto tiles = reinterpret_cast<vec(*)[FRAGS][WAVE]>(smem);
   int32_t* pt = reinterpret_cast<int32_t*>(smem + (size_t)RULED_BUFFERS * FRAGS * WAVE * 16);
-  __shared__ GroupRanges s_group[RULED_WAVES];
+  __shared__ GroupRanges s_group[WAVES];
   __shared__ int32_t s_odd;      // some value that is not finite was replaced
-  const Plan plan = make_plan<E, RULED_ROWS, Rule>(a);
+  const Plan plan = make_plan<E, ROWS, Rule>(a);
   if (blockIdx.x >= plan.total) return;
   const Piece c = piece_by_heads(plan, blockIdx.x, a.geom.n_heads);
-  const int tile0 = Rule::first_tile(a, c.base) / 2;      // of 64 keys
-  const int tok0 = a.tok.span.off[c.seq], row0 = c.group * RULED_ROWS, n_rows = (a.tok.span.off[c.seq + 1] - tok0) * a.group - row0;
+  const int tile0 = Rule::first_tile(a, c.base) / NT;      // of KEYS
+  const int tok0 = a.tok.span.off[c.seq], row0 = c.group * ROWS, n_rows = (a.tok.span.off[c.seq + 1] - tok0) * a.group - row0;
   const int n_keys = c.base + a.tok.span.off[c.seq + 1] - tok0, last_page = (n_keys - 1) / PAGE - STEPS * tile0;
   if (!a.whole) note_cut(a, plan, c, blockIdx.x, row0);
   {
     const int32_t* pages = a.tok.page_table + (int64_t)c.seq * a.tok.pt_stride + STEPS * tile0;
-    for (int i = threadIdx.x; i <= last_page; i += RULED_WAVES * WAVE) pt[i] = safe_page(a.geom, pages[i]);
+    for (int i = threadIdx.x; i <= last_page; i += WAVES * WAVE) pt[i] = safe_page(a.geom, pages[i]);
   }
   const int row = row0 + min(wave * TILE + col, n_rows - 1), tok = tok0 + row / a.group, q_head = c.head * a.group + row % a.group;
-  Rule rule;
-  rule.start_row(a, c.seq, tok, c.base + tok - tok0, q_head, n_keys);
   vec q[DSTEPS];
   {
     const E* qrow = (const E*)a.q + (int64_t)tok * a.q_stride + q_head * HD + half * G;
 #pragma unroll
     for (int s = 0; s < DSTEPS; ++s) q[s] = load16<E>(qrow + s * KS);
   }
+  Rule rule;
+  rule.start_row(a, c.seq, tok, c.base + tok - tok0, q_head, n_keys);
   GroupRanges group;
   group.take(rule.see);
   group.join_columns();
@@ -75,7 +85,7 @@ __global__ __launch_bounds__(RULED_WAVES * WAVE, 2) void ruled_rows_kernel(Atten
   if (threadIdx.x == 0) s_odd = 0;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < RULED_WAVES; ++w) group.join(s_group[w]);
+  for (int w = 0; w < WAVES; ++w) group.join(s_group[w]);
   TileWalk walk;
   walk.start(group, tile0, (n_keys + KEYS - 1) / KEYS, KEYS);
   const int all = walk.tiles(), i0 = all * c.part / c.parts, i1 = all * (c.part + 1) / c.parts, whole = walk.whole(), masked = min(whole, i1);
@@ -85,7 +95,9 @@ __global__ __launch_bounds__(RULED_WAVES * WAVE, 2) void ruled_rows_kernel(Atten
   float m_run = -INFINITY, l_run = 0.f, ref = 0.f;
   const float c2 = a.scale * LOG2E, to_log2 = rule.factor(c2);
   if (i0 < i1) {
-    vec next_k[K_MINE], next_v[V_MINE];
+    struct Fetched {
+      vec k[K_MINE], v[V_MINE];
+    };
     // Where this lane's pieces of a tile are: a page of its four and the place in it (keys past the last one are read from where they would
     // be, and masked).  A tile's number and pages are looked up a turn before its loads.
     const int k_page = wave * K_MINE / DSTEPS * 2 + PvStep<E>::key_of_row(col) / PAGE, v_page = wave * V_MINE / DT;
@@ -94,14 +106,14 @@ __global__ __launch_bounds__(RULED_WAVES * WAVE, 2) void ruled_rows_kernel(Atten
     const uint32_t page_elems = (uint32_t)a.geom.page_stride;
     auto tile_at = [&](int i) __attribute__((always_inline)) { return walk.tile(min(i, i1 - 1)); };
     auto page_at = [&](int kt, int page) __attribute__((always_inline)) { return (uint32_t)pt[min(STEPS * (kt - tile0) + page, last_page)]; };
-    auto fetch = [&](uint32_t of_k, uint32_t of_v) __attribute__((always_inline)) {
+    auto fetch = [&](Fetched& next, uint32_t of_k, uint32_t of_v) __attribute__((always_inline)) {
       const E *k = lane_k + (uint64_t)of_k * page_elems, *v = lane_v + (uint64_t)of_v * page_elems;
 #pragma unroll
-      for (int j = 0; j < K_MINE; ++j) next_k[j] = load16<E>(k + j * (PAGE * KS));
+      for (int j = 0; j < K_MINE; ++j) next.k[j] = load16<E>(k + j * (PAGE * KS));
 #pragma unroll
-      for (int j = 0; j < V_MINE; ++j) next_v[j] = load16<E>(v + j * (TILE * PAGE));
+      for (int j = 0; j < V_MINE; ++j) next.v[j] = load16<E>(v + j * (TILE * PAGE));
     };
-    auto put = [&](int i, int kt) __attribute__((always_inline)) {
+    auto put = [&](Fetched& next, int i, int kt) __attribute__((always_inline)) {
       if (i >= masked) {
         // Values of a tile that not all rows see whole: those past the last key, which may hold anything, become 0, and so does what is no
         // finite number (rows that see it are found at the end).
@@ -109,42 +121,42 @@ __global__ __launch_bounds__(RULED_WAVES * WAVE, 2) void ruled_rows_kernel(Atten
         uint32_t most = 0;
 #pragma unroll
         for (int j = 0; j < V_MINE; ++j) {
-          u32x4 w = words_of<E>(next_v[j]);
+          u32x4 w = words_of<E>(next.v[j]);
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             w[k] &= ValueBits<E>::mask(k, valid);
             most = ValueBits<E>::larger(most, w[k]);
             w[k] = ValueBits<E>::finite(w[k]);
           }
-          next_v[j] = __builtin_bit_cast(vec, w);
+          next.v[j] = __builtin_bit_cast(vec, w);
         }
         if (ValueBits<E>::largest(most) >= ValueBits<E>::ODD) s_odd = 1;
       }
       // K as [row tile][k-step], V as [step][feature tile]
       auto& to = tiles[i & (RULED_BUFFERS - 1)];
 #pragma unroll
-      for (int j = 0; j < K_MINE; ++j) to[wave * K_MINE + j][lane] = next_k[j];
+      for (int j = 0; j < K_MINE; ++j) to[wave * K_MINE + j][lane] = next.k[j];
 #pragma unroll
-      for (int j = 0; j < V_MINE; ++j) to[KF + wave * V_MINE + j][lane] = next_v[j];
+      for (int j = 0; j < V_MINE; ++j) to[KF + wave * V_MINE + j][lane] = next.v[j];
     };
-    f32x16 s[2];
+    f32x16 s[NT];
     u32x4 pw[STEPS];
     // Scores of tile i to weights, and the reference maximum moved where a score passes it by more than SLACK.
     auto weigh = [&](int i, int kt) __attribute__((always_inline)) {
       constexpr float SLACK = 6.f;
 #pragma unroll
-      for (int n = 0; n < 2; ++n) rule.template scores<E>(s[n], c2, kt * KEYS + n * TILE, half);
+      for (int n = 0; n < NT; ++n) rule.template scores<E>(s[n], c2, kt * KEYS + n * TILE, half);
       if (i >= masked) {
         const int key0 = i < i1 ? kt * KEYS : INT32_MAX / 2;      // (that nobody sees)
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int v = 0; v < 16; ++v)
             if (!rule.sees(key0 + n * TILE + PvStep<E>::key_of_acc(v, half))) s[n][v] = -INFINITY;
       }
       float mx = s[0][0];
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int v = 0; v < 16; ++v) mx = larger(mx, s[n][v]);
       const float mt = both_halves_max(mx) * to_log2;
@@ -172,49 +184,54 @@ __global__ __launch_bounds__(RULED_WAVES * WAVE, 2) void ruled_rows_kernel(Atten
         }
       l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
     };
-    int kt[5];      // of tiles i .. i + 4
+    int kt[AHEAD + 1];      // of tiles i .. i + AHEAD
 #pragma unroll
-    for (int k = 0; k < 5; ++k) kt[k] = tile_at(i0 + k);
+    for (int k = 0; k <= AHEAD; ++k) kt[k] = tile_at(i0 + k);
+    Fetched next[SETS];
+    {
+      Fetched first[3];      // (all at once: there is no output to hold yet)
 #pragma unroll
-    for (int k = 0; k < 3; ++k) {
-      fetch(page_at(kt[k], k_page), page_at(kt[k], v_page));
-      put(i0 + k, kt[k]);
+      for (int k = 0; k < 3; ++k) fetch(first[k], page_at(kt[k], k_page), page_at(kt[k], v_page));
+#pragma unroll
+      for (int k = 0; k < SETS; ++k) fetch(next[k], page_at(kt[3 + k], k_page), page_at(kt[3 + k], v_page));
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int k = 0; k < 3; ++k) put(first[k], i0 + k, kt[k]);
     }
-    fetch(page_at(kt[3], k_page), page_at(kt[3], v_page));
-    uint32_t of_k = page_at(kt[4], k_page), of_v = page_at(kt[4], v_page);
+    uint32_t of_k = page_at(kt[AHEAD], k_page), of_v = page_at(kt[AHEAD], v_page);
     __syncthreads();
     constexpr int RD = 4;
     vec ring[RD];
-    auto k_frag = [&](int i, int f) __attribute__((always_inline)) { return tiles[i & (RULED_BUFFERS - 1)][f % 2 * DSTEPS + f / 2][lane]; };
-    zero_acc<2>(s);
+    auto k_frag = [&](int i, int f) __attribute__((always_inline)) { return tiles[i & (RULED_BUFFERS - 1)][f % NT * DSTEPS + f / NT][lane]; };
+    zero_acc<NT>(s);
 #pragma unroll
-    for (int f = 0; f < KF; ++f) mfma32(s[f % 2], k_frag(i0, f), q[f / 2]);
+    for (int f = 0; f < KF; ++f) mfma32(s[f % NT], k_frag(i0, f), q[f / NT]);
     weigh(i0, kt[0]);
 #pragma unroll
     for (int f = 0; f < RD; ++f) ring[f] = k_frag(i0 + 1, f);
     // the waves of the second half run a phase behind those of the first
-    if (wave >= RULED_WAVES / 2) __builtin_amdgcn_s_barrier();
-    for (int i = i0; i < i1; ++i) {
-      zero_acc<2>(s);
+    if (PHASES && wave >= WAVES / 2) __builtin_amdgcn_s_barrier();
+    auto turn = [&](int i, Fetched& next) __attribute__((always_inline)) {
+      zero_acc<NT>(s);
 #pragma unroll
       for (int f = 0; f < FRAGS; ++f) {
         const vec x = ring[f % RD];
         const int n = f + RD;
         if (n < FRAGS) ring[f % RD] = n < KF ? k_frag(i + 1, n) : tiles[i & (RULED_BUFFERS - 1)][n][lane];
         __builtin_amdgcn_sched_barrier(0);
-        if (f < KF) mfma32(s[f % 2], x, q[f / 2]);
+        if (f < KF) mfma32(s[f % NT], x, q[f / NT]);
         else mfma32(o[(f - KF) % DT], x, __builtin_bit_cast(vec, pw[(f - KF) / DT]));
       }
       __builtin_amdgcn_sched_barrier(0);
       // (this wave's reads have come in: its matrix instructions took them)
-      asm volatile("s_barrier" ::: "memory");
-      put(i + 3, kt[3]);
-      fetch(of_k, of_v);
+      if constexpr (PHASES) asm volatile("s_barrier" ::: "memory");
+      put(next, i + 3, kt[3]);
+      fetch(next, of_k, of_v);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) kt[k] = kt[k + 1];
-      kt[4] = tile_at(i + 5);
-      of_k = page_at(kt[4], k_page);
-      of_v = page_at(kt[4], v_page);
+      for (int k = 0; k < AHEAD; ++k) kt[k] = kt[k + 1];
+      kt[AHEAD] = tile_at(i + AHEAD + 1);
+      of_k = page_at(kt[AHEAD], k_page);
+      of_v = page_at(kt[AHEAD], v_page);
       weigh(i + 1, kt[0]);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -222,16 +239,20 @@ __global__ __launch_bounds__(RULED_WAVES * WAVE, 2) void ruled_rows_kernel(Atten
       // (all but the fragments just asked for: what this wave put is there)
       asm volatile("s_waitcnt lgkmcnt(4)\n\ts_barrier" ::: "memory");
       static_assert(RD == 4, "the count above");
+    };
+    for (int i = i0; i < i1; i += SETS) {
+      turn(i, next[0]);
+      if (SETS == 2 && i + 1 < i1) turn(i + 1, next[SETS - 1]);
     }
-    if (wave < RULED_WAVES / 2) __builtin_amdgcn_s_barrier();
+    if (PHASES && wave < WAVES / 2) __builtin_amdgcn_s_barrier();
   }
   // Rows with weight on a value that was replaced: products of the weights with its indicator, one kind (NaN, +inf, -inf) at a time, over
   // the tiles again, 32 keys of them at a time.
   __syncthreads();
   if (i0 < i1 && s_odd != 0) {
 #pragma unroll 1
-    for (int i = 2 * max(i0, whole); i < 2 * i1; ++i) {
-      const int key0 = walk.tile(i / 2) * KEYS + i % 2 * TILE;
+    for (int i = NT * max(i0, whole); i < NT * i1; ++i) {
+      const int key0 = walk.tile(i / NT) * KEYS + i % NT * TILE;
       const int key = key0 + PvStep<E>::key_of_row(col), page0 = key0 / PAGE - STEPS * tile0;
       const E* krow = kv + kv_k_index(a.geom, pt[min(page0 + PvStep<E>::key_of_row(col) / PAGE, last_page)], c.head, key % PAGE, 0) + half * G;
       f32x16 x[1];
@@ -273,23 +294,23 @@ __global__ __launch_bounds__(RULED_WAVES * WAVE, 2) void ruled_rows_kernel(Atten
         store_elems4<E>((E*)a.out + (int64_t)tok * a.out_stride + q_head * HD + t * TILE + acc_row(4 * g, half),
                         f32x4{o[t][4 * g] * inv, o[t][4 * g + 1] * inv, o[t][4 * g + 2] * inv, o[t][4 * g + 3] * inv});
   } else {
-    float* part = attend_part(a, c.slot + c.part, RULED_ROWS * (HD + 2));
+    float* part = attend_part(a, c.slot + c.part, ROWS * (HD + 2));
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
       for (int g = 0; g < 4; ++g)
         *reinterpret_cast<f32x4*>(part + at * HD + t * TILE + acc_row(4 * g, half)) =
             f32x4{o[t][4 * g], o[t][4 * g + 1], o[t][4 * g + 2], o[t][4 * g + 3]};
-    if (half == 0) *reinterpret_cast<float2*>(part + RULED_ROWS * HD + 2 * at) = float2{m_run, L};
+    if (half == 0) *reinterpret_cast<float2*>(part + ROWS * HD + 2 * at) = float2{m_run, L};
   }
 }
-template <class Rule, int HD> static void launch_ruled_rows(AttendArgs a, hipStream_t st) {
-  const AttendGrid g = attend_grid<bf16_t, RULED_ROWS>(a);
-  ruled_rows_kernel<Rule, HD><<<g.wgs, RULED_WAVES * WAVE, ruled_rows_lds<HD>(), st>>>(a, live_word());
-  launch_merge<bf16_t, HD, RULED_ROWS, true>(a, g.cut, st);
+template <class Rule, int HD, int WAVES> static void launch_ruled_rows(AttendArgs a, hipStream_t st) {
+  const AttendGrid g = attend_grid<bf16_t, WAVES * TILE>(a);
+  ruled_rows_kernel<Rule, HD, WAVES><<<g.wgs, WAVES * WAVE, ruled_rows_lds<HD, WAVES>(), st>>>(a, live_word());
+  launch_merge<bf16_t, HD, WAVES * TILE, true>(a, g.cut, st);
 }
-template <class Rule, int HD> static bool configure_ruled_rows() {
-  return hipFuncSetAttribute((const void*)ruled_rows_kernel<Rule, HD>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)ruled_rows_lds<HD>()) == hipSuccess;
+template <class Rule, int HD, int WAVES> static bool configure_ruled_rows() {
+  return hipFuncSetAttribute((const void*)ruled_rows_kernel<Rule, HD, WAVES>, hipFuncAttributeMaxDynamicSharedMemorySize, (int)ruled_rows_lds<HD, WAVES>()) == hipSuccess;
 }
 
 // Meetings of a row tile with a key tile, as far as the host can tell (the lengths are on the device): as if caches were full, half of a
@@ -304,18 +325,21 @@ static int64_t likely_meetings(const AttendArgs& a) {
   }
   return sum * a.geom.n_heads / (a.rule.first || a.rule.end ? 4 : 1);      // (documents: most of them are much shorter than the sequence)
 }
-// The form of many rows where a call has that many of them (counted in heads of 128 features).  Its workgroups are few and take 10 us to begin
-// and end; against two row tiles per workgroup, 16 heads unless stated, in us: a causal prompt of 1000 tokens (8 thousand meetings) 48 and
-// 33, of 2000 (32) 64 and 54, of 4000 (126) 125 and 143; 256 tokens behind 4096 (17) 48 and 32, 1024 behind 4096 (74) 73 and 74, 2048 behind
-// 4096 (165) 126 and 139, 512 behind 12000 (98) 84 and 85; 8 heads of 4 queries: 512 behind 2000 (36) 53 and 46, 2000 causal (63) 70 and 72; 8000
-// tokens in a window of 512 (67) 105 and 93, of 2048 (259) 189 and 210; four prompts of 1811 in documents of 301 (52) 106 and 94; 4 heads of 2 queries
-// and 64 features, 4000 causal (62) 64 and 57.
-constexpr int64_t RULED_MEETINGS = 5 << 14;
+// The forms of many rows where a call has that many of them (counted in heads of 128 features).  Their workgroups take 9 and 13 us to begin and end,
+// those of two row tiles 8, but those are twice as many and read keys twice and four times as often.  Two row tiles | WAVES = 4 | 8, all with
+// their joins, 16 heads unless stated, in us (thousands of meetings in front): 8, a causal prompt of 1000 tokens 32 | 38 | 48; 17, 256 tokens behind
+// 4096 32 | 42 | 49; 32, 2000 causal 54 | 55 | 64; 36, 512 behind 2000, 8 heads of 4 queries 45 | 47 | 52; 37, 512 behind 4096 45 | 52 | 56; 52,
+// four prompts of 1811 in documents of 301 94 | 82 | 108; 63, 2000 causal, 8 heads of 4 queries 71 | 64 | 67; 67, 8000 in a window of 512 90 | 83 |
+// 108; 74, 1024 behind 4096 72 | 67 | 72; 98, 512 behind 12000 82 | 80 | 83; 126, 4000 causal 138 | 119 | 122; 192, 24 sequences of 17 to 32
+// behind 1000 to 8000, 8 heads of 4 queries 155 | 114 | 176; 259, 8000 in a window of 2048 202 | 169 | 183; 282, 6000 causal 255 | 204 | 202; 500, 8000
+// causal 404 | 309 | 298; 632, four of 2000 behind 4000 522 | 406 | 403; 1000, 8191 causal, 8 heads of 4 queries 752 | 596 | 544.
+constexpr int64_t RULED_FEW = 3 << 14, RULED_MANY = 25 << 14;
 template <class Rule, int HD> static void launch_ruled_t(bool bf16, const AttendArgs& a, hipStream_t st) {
   const int most = most_rows(a.tok.span, a.group);
   if (!bf16) launch_attend_t<float, HD, 1, 1, true, Rule>(a, st);
   else if (most <= TILE) launch_attend_t<bf16_t, HD, 1, 1, true, Rule>(a, st);
-  else if (most > 2 * TILE && likely_meetings(a) * HD >= RULED_MEETINGS * 128) launch_ruled_rows<Rule, HD>(a, st);
+  else if (most > 2 * TILE && likely_meetings(a) * HD >= RULED_MANY * 128) launch_ruled_rows<Rule, HD, 8>(a, st);
+  else if (most > 2 * TILE && likely_meetings(a) * HD >= RULED_FEW * 128) launch_ruled_rows<Rule, HD, 4>(a, st);
   else launch_attend_t<bf16_t, HD, 1, 2, true, Rule>(a, st);
 }
 template <class Rule> static void launch_ruled_hd(bool bf16, const AttendArgs& a, hipStream_t st) {
@@ -332,7 +356,7 @@ void launch_ruled(bool bf16, const AttendArgs& a, hipStream_t st) {
 
 template <class Rule, int HD> static bool configure_ruled_t() {
   return configure_attend_t<bf16_t, HD, 1, Rule>() && configure_attend_t<bf16_t, HD, 2, Rule>() && configure_attend_t<float, HD, 1, Rule>() &&
-         configure_ruled_rows<Rule, HD>();
+         configure_ruled_rows<Rule, HD, 4>() && configure_ruled_rows<Rule, HD, 8>();
 }
 template <class Rule> static bool configure_ruled_hd() { return configure_ruled_t<Rule, 64>() && configure_ruled_t<Rule, 128>(); }
 bool configure_ruled() {

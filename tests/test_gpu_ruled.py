@@ -246,7 +246,9 @@ def test_refusals(m):
 @pytest.mark.parametrize("dtype,nh,hd,G,lens,past,rule_name", [
     ("bf16", 16, 128, 1, [1100, 40, 0, 900], [300, 1500, 7, 0], "causal"), ("bf16", 8, 128, 4, [700, 333], [0, 1000], "block7"),
     ("bf16", 8, 64, 4, [1200, 900], [77, 500], "prefix_block"), ("bf16", 4, 128, 8, [600, 500], [900, 0], "all"),
-    ("bf16", 16, 128, 1, [2000, 1900], [0, 31], "documents"), ("bf16", 16, 128, 2, [800], [100], "prefix_window")])
+    ("bf16", 16, 128, 1, [2000, 1900], [0, 31], "documents"), ("bf16", 16, 128, 2, [800], [100], "prefix_window"),
+    ("bf16", 16, 128, 8, [3500], [300], "causal"), ("bf16", 16, 128, 8, [3600, 5], [300, 0], "documents"), ("bf16", 16, 64, 16, [3500], [301], "prefix_block"),
+    ("bf16", 16, 128, 8, [3500], [300], "prefix_window"), ("bf16", 16, 128, 8, [1800, 1700], [0, 300], "all")])
 def test_the_form_of_many_rows(m, dtype, nh, hd, G, lens, past, rule_name):
     """Calls that are large enough for it: a few tokens of them against the definition."""
     cache, ops = m
@@ -284,16 +286,18 @@ def test_the_form_of_many_rows(m, dtype, nh, hd, G, lens, past, rule_name):
                 got = out[t0 + i].cpu().double().view(-1, hd)[h]
                 e = 2 * e + 2.0 ** -19
                 bar = 2.0 ** -8 * ref.abs() + (2.0 ** -8 + e) * mag
-                assert (((got - ref).abs() <= bar) | (got == ref)).all(), (s, i, h, float((got - ref).abs().max()))
+                # float32 holds no weight below 2^-126 of the row's largest: it is 0, and 0 times a value that is not finite is no number
+                lost = ((w / w.max() < 2.0 ** -126)[:, None] & ~v[ok, h // G].isfinite()).any(0)
+                assert (((got - ref).abs() <= bar) | (got == ref) | lost).all(), (s, i, h, float((got - ref).abs().max()))
                 norm = float(torch.logsumexp(z[ok], 0))
                 assert abs(float(lse[t0 + i, h]) - norm) <= e + 2.0 ** -21 * abs(norm)
         t0 += n
     c.close()
 
 
-@pytest.mark.parametrize("lens,past", [([3, 40], [500, 0]), ([1300], [700])])
-def test_pages_beyond_32_bits(m, lens, past):
-    """The same rows in pages whose elements are numbered from 2^32 on (a pool of 8 GiB and more): the same bits, in both forms."""
+@pytest.mark.parametrize("lens,past,G", [([3, 40], [500, 0], 1), ([1300], [700], 1), ([4000], [300], 1), ([3500], [300], 8)])
+def test_pages_beyond_32_bits(m, lens, past, G):
+    """The same rows in pages whose elements are numbered from 2^32 on (a pool of 8 GiB and more): the same bits, in every form."""
     from paper_2510_08666_amd import binding
     cache, ops = m
     c = cache.Cache("bf16", 16, 128, lens, past, seed=3)
@@ -301,8 +305,8 @@ def test_pages_beyond_32_bits(m, lens, past):
     far = binding.Context(c.cfg, first + c.n_pages, c.ns, 64, c.max_pos)
     far.kv.view(torch.bfloat16).view(first + c.n_pages, -1)[first:].copy_(c.pool.view(c.n_pages, -1))
     far.kv.view(torch.bfloat16).view(first + c.n_pages, -1)[:c.n_pages].zero_()
-    q = c.randn(c.T, 2048)
-    outs = [torch.zeros(c.T, 2048, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    q = c.randn(c.T, G * 2048)
+    outs = [torch.zeros(c.T, G * 2048, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
     for ctx, table, out in ((c.ctx, c.d_table, outs[0]), (far, torch.where(c.d_table >= 0, c.d_table + first, c.d_table), outs[1])):
         ctx.attend_ruled(0, c.lens, c.d_past, table, q, out, block=1)
     torch.cuda.synchronize()
