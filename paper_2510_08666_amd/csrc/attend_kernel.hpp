@@ -265,6 +265,19 @@ template <bool CAP, bool BIAS> struct RangeRule {
   __device__ bool sees(int key) const {
     return (uint32_t)(key - see.a0) < (uint32_t)(see.a1 - see.a0) || (uint32_t)(key - see.b0) < (uint32_t)(see.b1 - see.b0);
   }
+  // Scores of keys that a row does not see become -inf.
+  template <typename E> __device__ void hide(f32x16& s, int key0, int half) const {
+    const int first = key0 + half * PvStep<E>::key_of_acc(0, 1);
+    if (__builtin_amdgcn_ballot_w64(see.a1 > see.a0)) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        if (!sees(first + PvStep<E>::key_of_acc(v, 0))) s[v] = -INFINITY;
+    } else {
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        if ((uint32_t)(first - see.b0 + PvStep<E>::key_of_acc(v, 0)) >= (uint32_t)(see.b1 - see.b0)) s[v] = -INFINITY;
+    }
+  }
   // cap * tanh(z / cap) = cap - 2 cap / (exp(2 z / cap) + 1): off by a few 2^-24 of cap, as the exponential and the reciprocal are
   __device__ float score(float s, float c2, float key) const {
     if constexpr (CAP) {
@@ -465,8 +478,11 @@ __global__ __launch_bounds__(ATTEND_WAVES * WAVE, (attend_waves_per_simd<E, HD>(
   float m_run = -INFINITY, l_run = 0.f;
   uint64_t marks[3] = {0, 0, 0};        // outputs (16 * t + v) that take in a NaN, an infinity, a negative one
   // One key tile; the next one's K loads are issued as soon as the scores have been worked out, its V loads behind the output products
-  // (clamped, so that no branch surrounds loads: a wave's last turn repeats its tile).  tail: a tile with new tokens, or the ragged end.
-  auto use_tile = [&](int kt, int next, auto tail) {
+  // (clamped, so that no branch surrounds loads: a wave's last turn repeats its tile).  A tile with new tokens, or the ragged end, is not WHOLE;
+  // what is no finite number among its values is looked for if it is ODD.
+  enum { WHOLE, PARTLY, ODD };
+  auto use_tile = [&](int kt, int next, auto kind) __attribute__((always_inline)) {
+    constexpr int KIND = decltype(kind)::value;
     asm volatile("" ::: "memory");      // keeps the query reads inside the loop
     f32x16 s[1];
     zero_acc<1>(s);
@@ -488,16 +504,17 @@ __global__ __launch_bounds__(ATTEND_WAVES * WAVE, (attend_waves_per_simd<E, HD>(
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (Rule::RANGES) rule.template scores<E>(s[0], c2, kt * TILE, half);
     bool odd = false;                   // some value of a new token is no finite number
-    if constexpr (decltype(tail)::value) {
+    if constexpr (KIND != WHOLE) {
       // what a row does not see scores -inf, values past the last key (which may hold anything) become 0
+      if constexpr (Rule::RANGES) rule.template hide<E>(s[0], kt * TILE, half);
+      else {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int key = kt * TILE + PvStep<E>::key_of_acc(i, half);
-        if constexpr (Rule::RANGES) {
-          if (!rule.sees(key)) s[0][i] = -INFINITY;
-        } else if (key >= n_keys || !sees(word, masked, key - c.base)) s[0][i] = -INFINITY;
+        for (int i = 0; i < 16; ++i) {
+          const int key = kt * TILE + PvStep<E>::key_of_acc(i, half);
+          if (key >= n_keys || !sees(word, masked, key - c.base)) s[0][i] = -INFINITY;
+        }
       }
-      if constexpr (PV) {
+      if (PV && (KIND == ODD || kt * TILE + TILE > n_keys)) {
         uint32_t most = 0;
 #pragma unroll
         for (int s2 = 0; s2 < STEPS; ++s2) {
@@ -510,10 +527,11 @@ __global__ __launch_bounds__(ATTEND_WAVES * WAVE, (attend_waves_per_simd<E, HD>(
             const u32x4 w = words_of<E>(v[s2][t]) & m;
             v[s2][t] = __builtin_bit_cast(vec, w);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) most = ValueBits<E>::larger(most, w[j]);
+            for (int j = 0; j < 4; ++j)
+              if constexpr (KIND == ODD) most = ValueBits<E>::larger(most, w[j]);
           }
         }
-        odd = masked && __builtin_amdgcn_ballot_w64(ValueBits<E>::largest(most) >= ValueBits<E>::ODD) != 0;
+        odd = KIND == ODD && masked && __builtin_amdgcn_ballot_w64(ValueBits<E>::largest(most) >= ValueBits<E>::ODD) != 0;
       }
     }
     float p[1][16];
@@ -528,7 +546,7 @@ __global__ __launch_bounds__(ATTEND_WAVES * WAVE, (attend_waves_per_simd<E, HD>(
         if constexpr (ONE) pv[s2][0] = PvStep<E>::p_vec(p[0], s2, 0);
         else PvWeights<E>::split(p[0], s2, pv[s2]);
       }
-      if (decltype(tail)::value && odd) {
+      if (KIND == ODD && odd) {
         // 0 * NaN would reach the rows that do not see the key: the product takes 0 in such a value's place, and the rows with
         // weight on it are found by products with its indicator, one kind (NaN, +inf, -inf) at a time, and marked
 #pragma unroll
@@ -571,21 +589,39 @@ __global__ __launch_bounds__(ATTEND_WAVES * WAVE, (attend_waves_per_simd<E, HD>(
     }
   };
   if constexpr (Rule::RANGES) {
-    const int all = rule.walk.tiles(), n = all * (c.part + 1) / c.parts, whole = min(n, rule.walk.whole());
-    int i = all * c.part / c.parts + team;
-    if (i < n && rt * TILE < n_rows) {
-      int kt = rule.walk.tile(i);
+    const int all = rule.walk.tiles(), n = all * (c.part + 1) / c.parts, whole = min(n, rule.walk.whole()), i0 = all * c.part / c.parts + team;
+    if (i0 < n && rt * TILE < n_rows) {
+      int i = i0, kt = rule.walk.tile(i);
       load_k(kt);
       load_v(kt);
-      auto walk = [&](int end, auto tail) {
+      auto walk = [&](int end, auto kind) __attribute__((always_inline)) {
         for (; i < end; i += TEAMS) {
           const int next = rule.walk.tile(min(i + TEAMS, n - 1));
-          use_tile(kt, next, tail);
+          use_tile(kt, next, kind);
           kt = next;
         }
       };
-      walk(whole, std::false_type{});
-      walk(n, std::true_type{});
+      walk(whole, std::integral_constant<int, WHOLE>{});
+      if (i < n) {
+        walk(n, std::integral_constant<int, PARTLY>{});
+        // Values that are not finite, also where a row does not see them (0 times them is no number), have left outputs that are not: once
+        // more with a look for them, which takes half as long again as a partly seen tile without it.
+        bool odd = false;
+        if constexpr (PV) {
+#pragma unroll
+          for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) odd |= !(fabsf(o[t][v]) < INFINITY);
+        }
+        if (__builtin_amdgcn_ballot_w64(odd)) {
+          zero_acc<DT>(o);
+          m_run = -INFINITY, l_run = 0.f;
+          i = i0, kt = rule.walk.tile(i);
+          load_k(kt);
+          load_v(kt);
+          walk(n, std::integral_constant<int, ODD>{});
+        }
+      }
     }
   } else {
     int kt = kt0 + team;
@@ -593,8 +629,8 @@ __global__ __launch_bounds__(ATTEND_WAVES * WAVE, (attend_waves_per_simd<E, HD>(
       const int full = min(c.base / TILE, kt1);
       load_k(kt);
       load_v(kt);
-      for (; kt < full; kt += TEAMS) use_tile(kt, min(kt + TEAMS, last_tile), std::false_type{});
-      for (; kt <= last_tile; kt += TEAMS) use_tile(kt, min(kt + TEAMS, last_tile), std::true_type{});
+      for (; kt < full; kt += TEAMS) use_tile(kt, min(kt + TEAMS, last_tile), std::integral_constant<int, WHOLE>{});
+      for (; kt <= last_tile; kt += TEAMS) use_tile(kt, min(kt + TEAMS, last_tile), std::integral_constant<int, ODD>{});
     }
   }
   if constexpr (PV) {

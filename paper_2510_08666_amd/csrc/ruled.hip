@@ -5,11 +5,12 @@
 //
 // Bound: the matrix instructions of the pairs that are seen (4 * head_dim operations each, at the 1.23 PFLOP/s of a large matrix product) or, for
 // few rows, one read of the keys and values.  Few rows take the kernel of attend_kernel.hpp with RangeRule for its words: a token behind
-// 511 positions 10.2 us (the chain of dependent loads), 48 tokens behind 1000 to 8000 in a window of 4097 with 8 heads of 4 queries 135 us (4.9 TB/s),
+// 511 positions 10.2 us (the chain of dependent loads), 48 tokens behind 1000 to 8000 in a window of 4097 with 8 heads of 4 queries 130 us (5.1 TB/s),
 // 512 tokens behind 4096, causal by blocks of 32, 39.9 us (0.46 PFLOP/s), prompts of 333 to 1811 tokens in documents of 301 with capped scores
-// 59 us (0.17 PFLOP/s: groups of rows in two documents walk both, all tiles partly seen, and end last).  Two row tiles hold their weights as one bfloat16 number (off by 2^-9 at most), which takes half
+// 47 us (0.22 PFLOP/s: groups of rows in two documents walk both, all tiles partly seen, and end last).  Two row tiles hold their weights as one bfloat16 number (off by 2^-9 at most), which takes half
 // as many matrix instructions out of the product with the values: 47.0 -> 43.2 us and 63.6 -> 60.2 with the joins; one row tile waits for
-// memory and keeps two.
+// memory and keeps two.  In tiles that are partly seen, values that are not finite are looked for only where an output has come out so, in a
+// second walk: 60.3 -> 47.6 us for the documents, 43.9 -> 41.9 for the chunk.
 #include "attend_kernel.hpp"
 
 namespace dinfer {
@@ -149,10 +150,7 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void ruled_rows_kernel(AttendArgs 
       if (i >= masked) {
         const int key0 = i < i1 ? kt * KEYS : INT32_MAX / 2;      // (that nobody sees)
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int v = 0; v < 16; ++v)
-            if (!rule.sees(key0 + n * TILE + PvStep<E>::key_of_acc(v, half))) s[n][v] = -INFINITY;
+        for (int n = 0; n < NT; ++n) rule.template hide<E>(s[n], key0 + n * TILE, half);
       }
       float mx = s[0][0];
 #pragma unroll
@@ -323,16 +321,16 @@ static int64_t likely_meetings(const AttendArgs& a) {
     if (a.rule.window > 0 && !a.rule.prefix) keys = keys < a.rule.window * (a.rule.block > 0 ? 1 : 2) + TILE ? keys : a.rule.window * (a.rule.block > 0 ? 1 : 2) + TILE;
     sum += ((int64_t)len * a.group + TILE - 1) / TILE * ((keys + TILE - 1) / TILE);
   }
-  return sum * a.geom.n_heads / (a.rule.first || a.rule.end ? 4 : 1);      // (documents: most of them are much shorter than the sequence)
+  return sum * a.geom.n_heads / (a.rule.first || a.rule.end ? 8 : 1);      // (documents: most of them are much shorter than the sequence)
 }
 // The forms of many rows where a call has that many of them (counted in heads of 128 features).  Their workgroups take 9 and 13 us to begin and end,
 // those of two row tiles 8, but those are twice as many and read keys twice and four times as often.  Two row tiles | WAVES = 4 | 8, all with
-// their joins, 16 heads unless stated, in us (thousands of meetings in front): 8, a causal prompt of 1000 tokens 32 | 38 | 48; 17, 256 tokens behind
-// 4096 32 | 42 | 49; 32, 2000 causal 54 | 55 | 64; 36, 512 behind 2000, 8 heads of 4 queries 45 | 47 | 52; 37, 512 behind 4096 45 | 52 | 56; 52,
-// four prompts of 1811 in documents of 301 94 | 82 | 108; 63, 2000 causal, 8 heads of 4 queries 71 | 64 | 67; 67, 8000 in a window of 512 90 | 83 |
-// 108; 74, 1024 behind 4096 72 | 67 | 72; 98, 512 behind 12000 82 | 80 | 83; 126, 4000 causal 138 | 119 | 122; 192, 24 sequences of 17 to 32
-// behind 1000 to 8000, 8 heads of 4 queries 155 | 114 | 176; 259, 8000 in a window of 2048 202 | 169 | 183; 282, 6000 causal 255 | 204 | 202; 500, 8000
-// causal 404 | 309 | 298; 632, four of 2000 behind 4000 522 | 406 | 403; 1000, 8191 causal, 8 heads of 4 queries 752 | 596 | 544.
+// their joins, 16 heads unless stated, in us (thousands of meetings in front): 8, a causal prompt of 1000 tokens 32 | 37 | 45; 17, 256 tokens behind
+// 4096 32 | 42 | 47; 26, four prompts of 1811 in documents of 301 74 | 79 | 98; 32, 2000 causal 54 | 54 | 61; 36, 512 behind 2000, 8 heads of 4
+// queries 45 | 48 | 50; 37, 512 behind 4096 44 | 51 | 53; 63, 2000 causal, 8 heads of 4 queries 71 | 61 | 67; 67, 8000 in a window of 512 83 | 82 |
+// 98; 74, 1024 behind 4096 74 | 69 | 70; 98, 512 behind 12000 85 | 82 | 82; 126, 4000 causal 141 | 113 | 119; 192, 24 sequences of 17 to 32
+// behind 1000 to 8000, 8 heads of 4 queries 148 | 115 | 175; 259, 8000 in a window of 2048 200 | 172 | 178; 282, 6000 causal 256 | 194 | 196; 500, 8000
+// causal 404 | 316 | 296; 632, four of 2000 behind 4000 533 | 409 | 384; 1000, 8191 causal, 8 heads of 4 queries 778 | 592 | 552.
 constexpr int64_t RULED_FEW = 3 << 14, RULED_MANY = 25 << 14;
 template <class Rule, int HD> static void launch_ruled_t(bool bf16, const AttendArgs& a, hipStream_t st) {
   const int most = most_rows(a.tok.span, a.group);

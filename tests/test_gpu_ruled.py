@@ -247,7 +247,7 @@ def test_refusals(m):
     ("bf16", 16, 128, 1, [1100, 40, 0, 900], [300, 1500, 7, 0], "causal"), ("bf16", 8, 128, 4, [700, 333], [0, 1000], "block7"),
     ("bf16", 8, 64, 4, [1200, 900], [77, 500], "prefix_block"), ("bf16", 4, 128, 8, [600, 500], [900, 0], "all"),
     ("bf16", 16, 128, 1, [2000, 1900], [0, 31], "documents"), ("bf16", 16, 128, 2, [800], [100], "prefix_window"),
-    ("bf16", 16, 128, 8, [3500], [300], "causal"), ("bf16", 16, 128, 8, [3600, 5], [300, 0], "documents"), ("bf16", 16, 64, 16, [3500], [301], "prefix_block"),
+    ("bf16", 16, 128, 8, [3500], [300], "causal"), ("bf16", 16, 128, 8, [3600, 5], [300, 0], "documents"), ("bf16", 16, 128, 16, [3700], [300], "documents"), ("bf16", 16, 64, 16, [3500], [301], "prefix_block"),
     ("bf16", 16, 128, 8, [3500], [300], "prefix_window"), ("bf16", 16, 128, 8, [1800, 1700], [0, 300], "all")])
 def test_the_form_of_many_rows(m, dtype, nh, hd, G, lens, past, rule_name):
     """Calls that are large enough for it: a few tokens of them against the definition."""
