@@ -456,7 +456,8 @@ int dinfer_attend_ruled(dinfer_ctx* ctx, int32_t layer, int32_t n_seq, const int
  *             fewer: -1 (d_score_out -infinity).
  *   d_score_out [n_seq][n_keep] out; may not be d_score.
  *   d_scratch 256-byte aligned, dinfer_beam_scratch_bytes (0: a size out of range), contents irrelevant.
- * Scores are compared in 64 bits and rounded once.  (Thousands of candidates with one and the same score at the border of the best n_keep
+ * Scores are compared in 64 bits and rounded once, whatever the logits' size; a row's sum of exponentials is float32's, within 2^-20 of
+ * itself.  (A score below float32's range is no candidate.  Thousands of candidates with one and the same score at the border of the best n_keep
  * take n_keep passes over them: right, but slow.)  n_keep <= 64, n_rows <= 1024, n_seq * n_rows <= 65535, vocab <= 2^24. */
 size_t dinfer_beam_scratch_bytes(int32_t n_seq, int32_t n_rows, int32_t vocab, int32_t n_keep);
 int dinfer_beam_select(const void* d_logits, int32_t dtype, int64_t row_stride, int32_t n_seq, int32_t n_rows, int32_t vocab,

@@ -96,16 +96,17 @@ __global__ __launch_bounds__(SELECT_THREADS) void select_chunk_kernel(SelectArgs
     float top = -INFINITY;
 #pragma unroll
     for (int r = 0; r < CHUNK_VALUES; ++r) top = fmaxf(top, x.raw(r));      // (the larger of a number and NaN is the number)
-    const float M = wave_largest(top), shift = M > -INFINITY ? M * 1.44269504088896341f : 0.f;
+    // (the maximum is taken off first: the largest term is 1 whatever the logits' size, and the sum between 1 and CHUNK)
+    const float M = wave_largest(top), away = M > -INFINITY ? M : 0.f;
     float sum = 0.f;
 #pragma unroll
-    for (int r = 0; r < CHUNK_VALUES; ++r) sum += __builtin_amdgcn_exp2f(fmaf(x.raw(r), 1.44269504088896341f, -shift));
+    for (int r = 0; r < CHUNK_VALUES; ++r) sum += __builtin_amdgcn_exp2f((x.raw(r) - away) * 1.44269504088896341f);
     sum = wave_total(sum);
     if (!(sum < INFINITY)) {      // NaN among them, or infinities, which count one each
       sum = 0.f;
 #pragma unroll
       for (int r = 0; r < CHUNK_VALUES; ++r)
-        sum += M < INFINITY ? __builtin_amdgcn_exp2f(fmaf(x.value(r), 1.44269504088896341f, -shift)) : x.value(r) == M ? 1.f : 0.f;
+        sum += M < INFINITY ? __builtin_amdgcn_exp2f((x.value(r) - away) * 1.44269504088896341f) : x.value(r) == M ? 1.f : 0.f;
       sum = wave_total(sum);
     }
     if (lane == 0) state[row * chunks + chunk] = ChunkState{M, sum};
@@ -129,7 +130,9 @@ __global__ __launch_bounds__(JOIN_THREADS) void select_join_kernel(SelectArgs a,
   const int seq = blockIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, K = a.n_keep, R = a.n_rows;
   const int64_t row0 = (int64_t)seq * R;
   state += row0 * chunks;
-  __shared__ double norm[MAX_SELECT_ROWS];      // score - log(sum of exp z); of rows that hold: the score
+  // score - log(sum of exp(z - peak)), which a candidate's z - peak is added to (peak itself may be so large that 64 bits lose the rest next to
+  // it); of rows that hold: the score
+  __shared__ double norm[MAX_SELECT_ROWS];
   __shared__ float peak[MAX_SELECT_ROWS];       // largest logit of the row, -inf: no candidate, NaN: one that is held
   __shared__ float row_sum[MAX_SELECT_ROWS];
   __shared__ __align__(16) Candidate list[JOIN_LIST];
@@ -143,7 +146,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void select_join_kernel(SelectArgs a,
   auto head = [](double n, float p, float m, bool first) {
     if (p != p) return first ? (float)n : -INFINITY;
     if (!(p > -INFINITY) || !(m > -INFINITY)) return -INFINITY;
-    return p < INFINITY ? (float)(n + (double)m) : m == INFINITY ? (float)n : -INFINITY;
+    return p < INFINITY ? (float)(n + ((double)m - (double)p)) : m == INFINITY ? (float)n : -INFINITY;
   };
   // A batch of rows: maximum and sum of each (a wave has JOIN_ROWS of them), the normalisers a lane per row.
   for (int b0 = 0; b0 < R; b0 += JOIN_WAVES * JOIN_ROWS) {
@@ -188,7 +191,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void select_join_kernel(SelectArgs a,
       const bool live = fabsf(base) < INFINITY, held = live && a.hold && hold >= 0, some = live && !held && p > -INFINITY;
       peak[mine] = held ? __builtin_nanf("") : some ? p : -INFINITY;
       // (infinite logits share the row's weight: log(1 / their number) each)
-      norm[mine] = held ? (double)base : some ? (double)base - ((p < INFINITY ? (double)p : 0.0) + log((double)row_sum[mine])) : 0.0;
+      norm[mine] = held ? (double)base : some ? (double)base - log((double)row_sum[mine]) : 0.0;
     }
     __syncthreads();
   }
@@ -288,13 +291,13 @@ __global__ __launch_bounds__(JOIN_THREADS) void select_join_kernel(SelectArgs a,
       return;
     }
     // (a logit below `cut` cannot; those above it are looked at)
-    const float cut = p < INFINITY ? (float)(bound - n - (fabs(bound) + fabs(n) + 1.0) * 0x1p-20) : INFINITY;
+    const float cut = p < INFINITY ? (float)((double)p + (bound - n) - (fabs(bound) + fabs(n) + fabs((double)p) + 1.0) * 0x1p-20) : INFINITY;
 #pragma unroll
     for (int v = 0; v < CHUNK_VALUES; ++v) {
       const float z = x.value(v);
       const bool may = z >= cut && z > -INFINITY;
       if (__builtin_amdgcn_ballot_w64(may)) {
-        const double score = p < INFINITY ? n + (double)z : n;
+        const double score = p < INFINITY ? n + ((double)z - (double)p) : n;
         take(may && order_of((float)score) >= least, Candidate{score, (uint64_t)r << 32 | (uint32_t)ChunkOf<E>::token(chunk, lane, v)});
       }
     }
