@@ -429,7 +429,7 @@ int dinfer_refresh_block_scored(dinfer_ctx* ctx, int32_t n_seq, int32_t block_le
  *   window    0: no bound.
  *   d_prefix  [n_seq] or null (0): positions that all tokens of the sequence see, one another included.
  *   d_first, d_end [T] or null (0 | all): the token's document, as cache positions.
- *   cap       0, or > 0: scores z become cap * tanh(z / cap).  At least 1e-30.
+ *   cap       0, or > 0: scores z become cap * tanh(z / cap), within 2^-20 of themselves whatever the cap.  At least 1e-30.
  *   d_slope   [n_q_heads] float32 or null: slope * |p - j| is taken off the head's scores (behind the cap). */
 typedef struct {
   int32_t block, window;

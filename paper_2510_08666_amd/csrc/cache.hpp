@@ -75,7 +75,8 @@ struct AttendRule {
   int32_t block, window;
   const int32_t *prefix;      // [n_seq]
   const int32_t *first, *end; // [T]
-  float cap;
+  float cap;                  // 0: none
+  float cap_ratio, cap_most, cap_unit, cap_small[4];      // launch_ruled: CapScores
   const float* slope;         // [n_heads * group]
 };
 
@@ -101,7 +102,7 @@ size_t attend_part_bytes(bool bf16, int head_dim, int max_pos);
 // planes: of the queries (two: the forward's own bfloat16 queries, normalisers only).
 void launch_attend(bool bf16, int planes, const AttendArgs& a, hipStream_t st);
 // Under a.rule (a.visible null).
-void launch_ruled(bool bf16, const AttendArgs& a, hipStream_t st);
+void launch_ruled(bool bf16, AttendArgs a, hipStream_t st);
 
 struct ScoreArgs {
   CacheTokens tok;

@@ -344,8 +344,9 @@ template <class Rule> static void launch_ruled_hd(bool bf16, const AttendArgs& a
   if (a.geom.head_dim == 128) launch_ruled_t<Rule, 128>(bf16, a, st);
   else launch_ruled_t<Rule, 64>(bf16, a, st);
 }
-void launch_ruled(bool bf16, const AttendArgs& a, hipStream_t st) {
+void launch_ruled(bool bf16, AttendArgs a, hipStream_t st) {
   const bool cap = a.rule.cap > 0.f, bias = a.rule.slope != nullptr;
+  if (cap) CapScores::prepare(a.rule, a.scale);
   if (cap && bias) launch_ruled_hd<RangeRule<true, true>>(bf16, a, st);
   else if (cap) launch_ruled_hd<RangeRule<true, false>>(bf16, a, st);
   else if (bias) launch_ruled_hd<RangeRule<false, true>>(bf16, a, st);
