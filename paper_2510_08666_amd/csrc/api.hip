@@ -1273,7 +1273,7 @@ int dinfer_attend_ruled(dinfer_ctx* c, int32_t layer, int32_t n_seq, const int32
   // (no cache is longer than ATTN_MAX_PAGES pages: longer blocks and windows are the same as these)
   const int most = 2 * ATTN_MAX_PAGES * PAGE;
   a.rule = AttendRule{rule->block < most ? rule->block : most, rule->window < most ? rule->window : most, rule->d_prefix, rule->d_first,
-                      rule->d_end, rule->cap, 0.f, 0.f, 0.f, {}, rule->d_slope};
+                      rule->d_end, rule->cap, 0.f, 0.f, {}, rule->d_slope};
   if (a.tok.span.off[n_seq] == 0) return DINFER_OK;
   launch_ruled(c->bf16, a, (hipStream_t)stream);
   HIP_TRY(hipGetLastError());

@@ -242,47 +242,39 @@ struct TileWalk {
     return t;
   }
 };
-// cap * tanh(z / cap) of a product s, z = scale * s, in units of log 2.  u = s * ratio is z / cap, held within +-8.5, where tanh is within 2^-23
-// of 1; tanh(u) = u P(u^2) / Q(u^2), and u S(u^2) for |u| <= 1/2, with the coefficients that make the largest relative error least (2^-26.3 and 2^-26.0,
-// by Lawson's weighted least squares), 1 in front, so that a score far below its cap stays as it is.  In float32 2^-21.4 of the score, the reciprocal
-// included.  (A form by exp(2u) cancels near 0: it is off by 2^-22 of the cap.)  A wave takes the quotient where one of its scores is beyond half the cap:
-// prompts of 333 to 1811 tokens in documents of 301 48.7 us without such scores | 55.4 with them everywhere, 8191 causal tokens with 8 heads of 4
-// queries 716 | 998 (uncapped 545); the quotient alone 54.3 and 948.
+// cap * tanh(z / cap) of a product s, z = scale * s, in units of log 2, with u = s * ratio = z / cap.  Up to |u| = 1/2 tanh(u) = u S(u^2), 1 in front, so
+// that a score far below its cap stays as it is; S's other coefficients make the largest relative error least (2^-26, by Lawson's weighted least
+// squares).  Beyond, cap - 2 cap / (exp(2u) + 1), which would cancel near 0.  Either is within 2^-21 of the score.  A score alone decides which one
+// it takes (so that no other one reaches it); a wave works out the second form where one of its scores needs it: prompts of 333 to
+// 1811 tokens in documents of 301 48.2 us without | 54.3 with it everywhere, 8191 causal tokens with 8 heads of 4 queries 732 | 1000 (uncapped 545).
 struct CapScores {
-  static constexpr float MOST = 8.5f;
   static constexpr double S[4] = {-0.333331438954662, 0.13325878934223193, -0.0530454923870277, 0.017241486995792973};
-  static constexpr float P1 = 1.34158604e-1f, P2 = 3.53707961e-3f, P3 = 2.12994016e-5f, P4 = 1.43330474e-8f;
-  static constexpr float Q1 = 4.67491866e-1f, Q2 = 2.60344951e-2f, Q3 = 3.35377411e-4f, Q4 = 8.1718979e-7f;
-  // ratio: of a product to u; most: the largest product; unit: of a product to scores in log 2 (all of them finite, and ratio * cap = scale
-  // unless that ratio is beyond float32, where every product but 0 is at the cap)
+  // ratio: of a product to u, neither 0 nor infinite; unit: of a product to scores in log 2; small: S's coefficients, times unit
   static void prepare(AttendRule& r, float scale) {
-    const double ratio = (double)scale / r.cap, used = ratio < FLT_MAX ? ratio : FLT_MAX, most = MOST / used;
-    r.cap_ratio = (float)used;
-    r.cap_most = most < FLT_MAX ? (float)most : FLT_MAX;
+    const double ratio = (double)scale / r.cap, used = ratio < FLT_MAX ? ratio : FLT_MAX;      // (beyond: every product but 0 is at the cap)
+    r.cap_ratio = (float)used > FLT_TRUE_MIN ? (float)used : FLT_TRUE_MIN;
     r.cap_unit = (float)(used * r.cap * (double)LOG2E);
     for (int k = 0; k < 4; ++k) r.cap_small[k] = (float)(S[k] * used * r.cap * (double)LOG2E);
   }
-  float ratio, most, unit, small[4];      // small: S's coefficients, times unit
-  __device__ float score(float s) const {
-    s = __builtin_elementwise_minimum(__builtin_elementwise_maximum(s, -most), most);      // (NaN stays)
-    const float u = s * ratio, y = u * u;
-    const float p = fmaf(fmaf(fmaf(fmaf(P4, y, P3), y, P2), y, P1), y, 1.f), q = fmaf(fmaf(fmaf(fmaf(Q4, y, Q3), y, Q2), y, Q1), y, 1.f);
-    return s * unit * (p * __builtin_amdgcn_rcpf(q));
-  }
-  __device__ float small_score(float s) const {
-    const float u = s * ratio, y = u * u;
+  float cap2, ratio, unit, small[4];
+  __device__ float below(float s, float u) const {
+    const float y = u * u;
     return s * fmaf(fmaf(fmaf(fmaf(small[3], y, small[2]), y, small[1]), y, small[0]), y, unit);
   }
   __device__ f32x16 scores(f32x16 s) const {
     float top = 0.f;
 #pragma unroll
     for (int v = 0; v < 16; ++v) top = fmaxf(top, fabsf(s[v]));      // (NaN stays in either form)
-    if (__builtin_amdgcn_ballot_w64(top > most * (0.5f / MOST))) {
+    if (__builtin_amdgcn_ballot_w64(top * ratio > 0.5f)) {
 #pragma unroll
-      for (int v = 0; v < 16; ++v) s[v] = score(s[v]);
+      for (int v = 0; v < 16; ++v) {
+        const float u = s[v] * ratio, t = __builtin_amdgcn_exp2f(u * (2.f * LOG2E));
+        const float beyond = fmaf(__builtin_amdgcn_rcpf(t + 1.f), -2.f * cap2, cap2);
+        s[v] = fabsf(u) > 0.5f ? beyond : below(s[v], u);
+      }
     } else {
 #pragma unroll
-      for (int v = 0; v < 16; ++v) s[v] = small_score(s[v]);
+      for (int v = 0; v < 16; ++v) s[v] = below(s[v], s[v] * ratio);
     }
     return s;
   }
@@ -300,7 +292,7 @@ template <bool CAP, bool BIAS> struct RangeRule {
   __device__ void start_row(const AttendArgs& a, int seq, int tok, int p, int q_head, int n_keys) {
     see = row_ranges(a.rule, seq, tok, p, n_keys);
     if constexpr (BIAS) at = p, slope2 = a.rule.slope[q_head] * LOG2E;
-    if constexpr (CAP) cap = CapScores{a.rule.cap_ratio, a.rule.cap_most, a.rule.cap_unit, {a.rule.cap_small[0], a.rule.cap_small[1], a.rule.cap_small[2], a.rule.cap_small[3]}};
+    if constexpr (CAP) cap = CapScores{a.rule.cap * LOG2E, a.rule.cap_ratio, a.rule.cap_unit, {a.rule.cap_small[0], a.rule.cap_small[1], a.rule.cap_small[2], a.rule.cap_small[3]}};
   }
   __device__ void start(const AttendArgs& a, int seq, int tok, int p, int q_head, int n_keys, int kt0, int kt1) {
     start_row(a, seq, tok, p, q_head, n_keys);

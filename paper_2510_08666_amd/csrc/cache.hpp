@@ -76,7 +76,7 @@ struct AttendRule {
   const int32_t *prefix;      // [n_seq]
   const int32_t *first, *end; // [T]
   float cap;                  // 0: none
-  float cap_ratio, cap_most, cap_unit, cap_small[4];      // launch_ruled: CapScores
+  float cap_ratio, cap_unit, cap_small[4];      // launch_ruled: CapScores
   const float* slope;         // [n_heads * group]
 };
 

@@ -18,8 +18,8 @@ def cache_ops():
 
 def definition(c, q, group, cap, slope, scale):
     """out, lse, sum of p |v|, and a bound on a score's error that follows the scores and not the cap: (hd + 4) roundings of the product's
-    size, 2^-20 of the score for the cap (tanh as a quotient: within 2^-21.4 by itself, and the reciprocal, two products and the scale, half a step
-    each), three roundings of the bias."""
+    size, 2^-20 of the score for the cap (2^-21.1 at most: for tanh next to 1/2, where the exponential, the reciprocal and two sums lose a step each
+    of a number below 1; two products and the scale, half a step each), three roundings of the bias."""
     pool, nq, t, err = c.pool.cpu(), c.nh * group, 0, 0.0
     q = q.cpu().double().reshape(c.T, nq, c.hd)
     out, lse, mag = torch.zeros(c.T, nq, c.hd).double(), torch.zeros(c.T, nq).double(), torch.zeros(c.T, nq, c.hd).double()
@@ -97,3 +97,19 @@ def test_scores_at_the_cap_and_far_below_it(cache_ops, call):
     tiny, tiny_lse = attend(c, q, G, 1e-30, None, 1.6e38)      # weights alike
     assert (tiny_lse - n.log()).abs().max() <= 2.0 ** -19
     c.close()
+
+
+@pytest.mark.parametrize("cap", [5.0, 30.0])
+def test_a_capped_score_is_its_own(cache_ops, cap):
+    """What lies in keys that nobody sees, and behind the last one, however large, changes no bit."""
+    for dtype, nh, hd, G, lens, past in CALLS + [("bf16", 16, 128, 1, [2600], [300])]:
+        c = cache_ops.Cache(dtype, nh, hd, lens, past, seed=11)
+        q, total = c.randn(c.T, nh * G * hd, scale=1.5), lens[0] + past[0]
+        out, lse = (torch.zeros(2, c.T, nh * G * w, dtype=t, device=DEV) for w, t in ((hd, q.dtype), (1, torch.float32)))
+        first = torch.tensor([9] * c.T, dtype=torch.int32, device=DEV)
+        for turn in range(2):
+            c.ctx.attend_ruled(0, c.lens, c.d_past, c.d_table, q, out[turn], block=1, cap=cap, first=first, lse=lse[turn])
+            torch.cuda.synchronize()
+            c.set_rows(0, [0, 3, 8, total, total + 5], k=torch.full((5, nh, hd), 1e4))
+        assert torch.equal(out[0], out[1]) and torch.equal(lse[0], lse[1])
+        c.close()
