@@ -1332,20 +1332,16 @@ int dinfer_kv_fork(dinfer_ctx* c, int32_t n_old, int32_t n_new, const int32_t* d
     return fail(DINFER_EINVAL, "an output is an input");
   if (n_states < 0 || n_states > MAX_STATES || (n_states > 0 && !h_states)) return fail(DINFER_EINVAL, "%d states", n_states);
   ForkArgs a{};
-  int64_t groups = 2 * MAX_SEQS;
   for (int k = 0; k < n_states; ++k) {
     const dinfer_state& s = h_states[k];
     if (!s.d_out || (!s.d_in && n_old > 0) || s.d_in == s.d_out) return fail(DINFER_EINVAL, "state %d: null, or in place", k);
     if (s.row_bytes < 4 || s.row_bytes > INT32_MAX || (s.row_bytes | (uintptr_t)s.d_in | (uintptr_t)s.d_out) & 3)
       return fail(DINFER_EINVAL, "state %d: rows of %lld bytes", k, (long long)s.row_bytes);
     a.state[k] = StateRows{(const char*)s.d_in, (char*)s.d_out, s.row_bytes};
-    groups += (s.row_bytes / 4096 + 1) * n_new;
   }
   int rc = check_pool(c);
   if (rc != DINFER_OK) return rc;
   a.pool = page_pool(c);
-  groups += ((int64_t)rewrite / PAGE + 2) * n_new * a.pool.n_layers * (a.pool.page_bytes / 4096 + 1);
-  if (groups > INT32_MAX) return fail(DINFER_EUNSUPPORTED, "too many pages to copy in one call");
   a.n_old = n_old, a.n_new = n_new;
   a.parent = d_parent, a.len = d_len, a.held = d_held;
   a.table = d_page_table, a.pt_stride = pt_stride;
@@ -1358,6 +1354,7 @@ int dinfer_kv_fork(dinfer_ctx* c, int32_t n_old, int32_t n_new, const int32_t* d
   a.new_refs = d_new_refs, a.missing = d_short;
   a.n_states = n_states;
   a.copies = at<CopyList>(c->ws, c->wsm.fork_copies);
+  if (!plan_fork(a)) return fail(DINFER_EUNSUPPORTED, "states too large for one call");
   launch_fork(a, (hipStream_t)stream);
   HIP_TRY(hipGetLastError());
   return DINFER_OK;

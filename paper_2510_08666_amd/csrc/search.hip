@@ -487,7 +487,6 @@ struct PageBits {
 };
 static size_t page_bits_bytes(int n_pages) { return (size_t)((n_pages + 63) / 64) * 12 + 16; }
 
-constexpr int PIECE_THREADS = 256, PIECE = PIECE_THREADS * 64;      // bytes that a workgroup moves at once, four loads of 16 per thread under way
 __device__ inline void move_piece(const char* from, char* to, int64_t bytes) {      // bytes: a multiple of 16
   u32x4 v[4];
 #pragma unroll
@@ -505,7 +504,6 @@ __device__ inline void move_page_piece(const PagePool& p, int from, int to, int 
   char* at = p.kv + layer * p.layer_bytes + (int64_t)piece * PIECE;
   move_piece(at + from * p.page_bytes, at + to * p.page_bytes, min((int64_t)PIECE, p.page_bytes - (int64_t)piece * PIECE));
 }
-static int page_pieces(const PagePool& p) { return (int)((p.page_bytes + PIECE - 1) / PIECE); }
 
 // ---------------------------------------------------------------- fork
 // What becomes of sequence i: columns below `own` are its parent's pages, shared; those below `need` are its own.
@@ -604,13 +602,9 @@ __global__ __launch_bounds__(POOL_THREADS) void fork_plan_kernel(ForkArgs a) {
 
 // The second: shared columns and the counts of all pages, the sequences' states, and the pages that are copied.  Bound by their bytes,
 // once each way: 64 sequences, 69 MB, 11.9 us.  (Workgroups that looked for themselves what to copy: 28.7 us both launches, with the list 25.0.)
-struct ForkGrid {
-  int state0, page0;          // first workgroups of the states and of the pages (in front: a row of the tables each)
-  int state_pieces[MAX_STATES];
-  int pieces;
-};
-__global__ __launch_bounds__(PIECE_THREADS) void fork_apply_kernel(ForkArgs a, ForkGrid g) {
+__global__ __launch_bounds__(PIECE_THREADS) void fork_apply_kernel(ForkArgs a) {
   if (*a.missing > 0) return;
+  const ForkGrid& g = a.grid;
   int b = blockIdx.x;
   if (b < a.n_new) {
     const Fork f = fork_of(a, b);
@@ -647,11 +641,15 @@ __global__ __launch_bounds__(PIECE_THREADS) void fork_apply_kernel(ForkArgs a, F
       for (int64_t j = threadIdx.x * 4; j < n; j += PIECE_THREADS * 4) *reinterpret_cast<uint32_t*>(to + j) = none ? 0u : *reinterpret_cast<const uint32_t*>(from + j);
     return;
   }
-  b -= g.page0;
-  const int piece = b % g.pieces, layer = b / g.pieces % a.pool.n_layers, copy = b / (g.pieces * a.pool.n_layers);
-  const int n = a.copies->n;
-  const int2 p = a.copies->page[copy];      // (as many as the launch has; beyond n: anything)
-  if (copy < n) move_page_piece(a.pool, p.x, p.y, layer, piece);
+  const int per = g.pieces * a.pool.n_layers;
+  int item = b - g.page0;
+  int2 p = a.copies->page[item / per];      // (there are as many as workgroups; beyond n: anything)
+  const int items = a.copies->n * per;      // (of different pages of the pool, at least 4 KiB each: below 2^31)
+  while (item < items) {
+    move_page_piece(a.pool, p.x, p.y, item / g.pieces % a.pool.n_layers, item % g.pieces);
+    item += g.page_groups;
+    if (item < items) p = a.copies->page[item / per];
+  }
 }
 
 // Columns of a sequence that hold something and are written: from (len - rewrite) / PAGE on.
@@ -660,18 +658,14 @@ static int fork_columns(int rewrite, int stride) {
   return n < stride ? n : stride;
 }
 size_t fork_copies_bytes(int max_seqs, int max_pos) { return sizeof(CopyList) + (size_t)max_seqs * fork_columns(max_pos, INT32_MAX) * sizeof(int2); }
+bool plan_fork(ForkArgs& a) {
+  int64_t row_bytes[MAX_STATES];
+  for (int k = 0; k < a.n_states; ++k) row_bytes[k] = a.state[k].row_bytes;
+  return fork_grid(a.n_old, a.n_new, row_bytes, a.n_states, fork_columns(a.rewrite, a.new_stride), a.pool.n_layers, a.pool.page_bytes, &a.grid);
+}
 void launch_fork(const ForkArgs& a, hipStream_t st) {
-  ForkGrid g{};
-  g.state0 = a.n_new + a.n_old;
-  g.page0 = g.state0;
-  for (int k = 0; k < a.n_states; ++k) {
-    g.state_pieces[k] = (int)((a.state[k].row_bytes + PIECE - 1) / PIECE);
-    g.page0 += g.state_pieces[k] * a.n_new;
-  }
-  const int columns = fork_columns(a.rewrite, a.new_stride);
-  g.pieces = page_pieces(a.pool);
   fork_plan_kernel<<<1, POOL_THREADS, page_bits_bytes(a.pool.n_pages), st>>>(a);
-  fork_apply_kernel<<<g.page0 + a.n_new * columns * a.pool.n_layers * g.pieces, PIECE_THREADS, 0, st>>>(a, g);
+  fork_apply_kernel<<<a.grid.page0 + a.grid.page_groups, PIECE_THREADS, 0, st>>>(a);
 }
 
 // ---------------------------------------------------------------- compact
@@ -726,7 +720,7 @@ __global__ __launch_bounds__(PIECE_THREADS) void compact_move_kernel(CompactArgs
 }
 constexpr int MOVE_GROUPS = 4096;
 void launch_compact(const CompactArgs& a, hipStream_t st) {
-  const int pieces = page_pieces(a.pool);
+  const int pieces = (int)pieces_of(a.pool.page_bytes);
   const int64_t most = (int64_t)(a.pool.n_pages / 2 + 1) * a.pool.n_layers * pieces;
   compact_plan_kernel<<<1, POOL_THREADS, page_bits_bytes(a.pool.n_pages), st>>>(a);
   compact_move_kernel<<<a.n_seq + (int)(most < MOVE_GROUPS ? most : MOVE_GROUPS), PIECE_THREADS, 0, st>>>(a, pieces);

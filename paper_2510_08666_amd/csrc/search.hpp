@@ -1,6 +1,7 @@
 // Operators of a search over several continuations: the best (row, token) pairs of a sequence's rows, sequences that fork from
 // parents and share their pages, and the move of the pages in use to the front of the pool.
 #pragma once
+#include "fork_plan.hpp"
 #include "kernels.hpp"
 
 namespace dinfer {
@@ -8,7 +9,6 @@ namespace dinfer {
 constexpr int MAX_KEEP = 64, MAX_SELECT_ROWS = 1024;
 // Bits of a pool's pages in LDS: 8 bytes and a count for every 64 of them.
 constexpr int MAX_POOL_PAGES = 12288 * 64;
-constexpr int MAX_STATES = 8;
 
 struct SelectArgs {
   const void* logits;         // [n_seq * n_rows] rows of vocab, row_stride elements apart
@@ -54,7 +54,10 @@ struct ForkArgs {
   StateRows state[MAX_STATES];
   int32_t n_states;
   CopyList* copies;           // fork_copies_bytes
+  ForkGrid grid;              // plan_fork
 };
+// The launch's shape; false: too large.
+bool plan_fork(ForkArgs& a);
 void launch_fork(const ForkArgs& a, hipStream_t st);
 
 struct CompactArgs {
