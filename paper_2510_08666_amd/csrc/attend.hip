@@ -269,7 +269,7 @@ static int64_t most_meetings(const AttendArgs& a) {
 // tiles could share: one tile per workgroup (3 sequences of 5 to 33 tokens 28.9 -> 20.4 us).
 constexpr int64_t ROWS_FORM_MEETINGS = 1 << 17;
 template <int HD> static void launch_attend_hd(bool bf16, int planes, const AttendArgs& a, hipStream_t st) {
-  const int most = most_rows(a.tok.span, a.group);
+  const int most = most_rows(a);
   if (bf16) {
     const bool rows_form = most > 2 * TILE && a.out && most_meetings(a) >= ROWS_FORM_MEETINGS;
     if (rows_form && most > 4 * TILE) launch_attend_rows<HD, 8>(a, st);

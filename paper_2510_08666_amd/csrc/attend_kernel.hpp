@@ -12,12 +12,10 @@ namespace dinfer {
 
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
 
-static int most_rows(const SeqSpan& span, int group) {
+static int rows_of(const AttendArgs& a, int s) { return (a.tok.span.off[s + 1] - a.tok.span.off[s]) * a.group; }
+static int most_rows(const AttendArgs& a) {
   int most = 0;
-  for (int s = 0; s < span.n_seq; ++s) {
-    const int rows = (span.off[s + 1] - span.off[s]) * group;
-    most = rows > most ? rows : most;
-  }
+  for (int s = 0; s < a.tok.span.n_seq; ++s) most = rows_of(a, s) > most ? rows_of(a, s) : most;
   return most;
 }
 
@@ -152,6 +150,7 @@ struct Plan {
 // WordRule: all keys in front of the new tokens, and of those the ones that a visibility word names.
 struct WordRule {
   static constexpr bool RANGES = false;
+  __host__ __device__ static bool takes(const AttendArgs&, int) { return true; }      // a sequence of so many rows
   __device__ static int first_tile(const AttendArgs&, int) { return 0; }
   __device__ float factor(float c2) const { return c2; }      // of the scores, to units of log 2
 };
@@ -281,6 +280,7 @@ struct CapScores {
 };
 template <bool CAP, bool BIAS> struct RangeRule {
   static constexpr bool RANGES = true;
+  __host__ __device__ static bool takes(const AttendArgs& a, int rows) { return a.rule.takes(rows); }
   // a window without a prefix lets a sequence's walk begin late
   __device__ static int first_tile(const AttendArgs& a, int base) {
     return a.rule.window > 0 && !a.rule.prefix ? max(0, base - a.rule.window + 1) / TILE : 0;
@@ -341,7 +341,7 @@ template <typename E, int ROWS, class Rule = WordRule> __device__ inline Plan ma
   Plan p;
   p.base = cache_base(a.tok, s, len);
   p.tiles = (p.base + len + TILE - 1) / TILE - Rule::first_tile(a, p.base);
-  p.groups = (len * a.group + ROWS - 1) / ROWS;
+  p.groups = Rule::takes(a, len * a.group) ? (len * a.group + ROWS - 1) / ROWS : 0;
   uint32_t pairs = p.groups * a.geom.n_heads;
   const uint32_t units = __builtin_amdgcn_readlane(lane_scan(pairs * p.tiles), WAVE - 1);      // (host: the sum stays below 2^31)
   const uint32_t all_pairs = __builtin_amdgcn_readlane(lane_scan(pairs), WAVE - 1);
@@ -796,9 +796,10 @@ template <typename E, int HD, int NP, int RG, bool PV> constexpr size_t attend_l
 struct AttendGrid {
   unsigned wgs, cut;
 };
-template <typename E, int ROWS> static AttendGrid attend_grid(AttendArgs& a) {
+template <typename E, int ROWS, class Rule = WordRule> static AttendGrid attend_grid(AttendArgs& a) {
   int64_t pairs = 0;
-  for (int s = 0; s < a.tok.span.n_seq; ++s) pairs += ((int64_t)(a.tok.span.off[s + 1] - a.tok.span.off[s]) * a.group + ROWS - 1) / ROWS;
+  for (int s = 0; s < a.tok.span.n_seq; ++s)
+    if (Rule::takes(a, rows_of(a, s))) pairs += ((int64_t)rows_of(a, s) + ROWS - 1) / ROWS;
   pairs *= a.geom.n_heads;
   a.whole = single_slice() || a.tok.limit <= min_cut<E>() * TILE;
   const int64_t wgs = a.whole ? pairs : pairs + resident(ROWS);
@@ -808,7 +809,7 @@ template <typename E, int HD, int ROWS, bool PV> static void launch_merge(const 
   if (cut > 0) attend_merge_kernel<E, HD, ROWS, PV><<<cut * (ROWS / (merge_rows<HD, PV>() * (ROWS > 64 ? 4 : 1))), MERGE_THREADS, 0, st>>>(a, live_word());
 }
 template <typename E, int HD, int NP, int RG, bool PV, class Rule = WordRule> static void launch_attend_t(AttendArgs a, hipStream_t st) {
-  const AttendGrid g = attend_grid<E, RG * TILE>(a);
+  const AttendGrid g = attend_grid<E, RG * TILE, Rule>(a);
   attend_kernel<E, HD, NP, RG, PV, Rule><<<g.wgs, ATTEND_WAVES * WAVE, attend_lds<E, HD, NP, RG, PV>(), st>>>(a, live_word());
   launch_merge<E, HD, RG * TILE, PV>(a, g.cut, st);
 }

@@ -78,6 +78,8 @@ struct AttendRule {
   float cap;                  // 0: none
   float cap_ratio, cap_unit, cap_small[4];      // launch_ruled: CapScores
   const float* slope;         // [n_heads * group]
+  int32_t least_rows, most_rows;      // of the sequences that a launch takes, set by launch_ruled
+  __host__ __device__ bool takes(int rows) const { return rows >= least_rows && rows <= most_rows; }
 };
 
 // Queries of one cache head's group are rows of one contraction: row r of a sequence is token r / group, query head

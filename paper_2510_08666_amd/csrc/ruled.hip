@@ -7,7 +7,7 @@
 // few rows, one read of the keys and values.  Few rows take the kernel of attend_kernel.hpp with RangeRule for its words: a token behind
 // 511 positions 10.2 us (the chain of dependent loads), 48 tokens behind 1000 to 8000 in a window of 4097 with 8 heads of 4 queries 130 us (5.1 TB/s),
 // 512 tokens behind 4096, causal by blocks of 32, 39.9 us (0.46 PFLOP/s), prompts of 333 to 1811 tokens in documents of 301 with capped scores
-// 47 us (0.22 PFLOP/s: groups of rows in two documents walk both, all tiles partly seen, and end last).  Two row tiles hold their weights as one bfloat16 number (off by 2^-9 at most), which takes half
+// 47 us (0.22 PFLOP/s: groups of rows in two documents walk both, all tiles partly seen, and end last).  Two row tiles hold their weights as one bfloat16 number (off by 2^-8 at most), which takes half
 // as many matrix instructions out of the product with the values: 47.0 -> 43.2 us and 63.6 -> 60.2 with the joins; one row tile waits for
 // memory and keeps two.  In tiles that are partly seen, values that are not finite are looked for only where an output has come out so, in a
 // second walk: 60.3 -> 47.6 us for the documents, 43.9 -> 41.9 for the chunk.
@@ -19,7 +19,7 @@ namespace dinfer {
 // all of them.  In a turn a wave multiplies (the next tile's keys with its queries, this tile's values with their weights, matrix
 // instructions that are fed from LDS without a pause), brings in its share of a later tile and works out the exponentials of the scores that
 // it multiplied.  Four buffers: V of tile i, K of tile i + 1, the first fragments of K of tile i + 2, tile i + 3 on its way in.  Weights enter
-// the product with the values as one bfloat16 number each, rounded to nearest (off by 2^-9 at most; the sum of a row is that of the
+// the product with the values as one bfloat16 number each, rounded to nearest (off by 2^-8 at most; the sum of a row is that of the
 // weights before): a second one would be half as many matrix instructions more.
 //
 // WAVES = 4: 128 rows, tiles of 32 keys, two workgroups per compute unit, whose waves on a SIMD cover each other as they come; loads are under way
@@ -303,7 +303,7 @@ __global__ __launch_bounds__(WAVES * WAVE, 2) void ruled_rows_kernel(AttendArgs 
   }
 }
 template <class Rule, int HD, int WAVES> static void launch_ruled_rows(AttendArgs a, hipStream_t st) {
-  const AttendGrid g = attend_grid<bf16_t, WAVES * TILE>(a);
+  const AttendGrid g = attend_grid<bf16_t, WAVES * TILE, Rule>(a);
   ruled_rows_kernel<Rule, HD, WAVES><<<g.wgs, WAVES * WAVE, ruled_rows_lds<HD, WAVES>(), st>>>(a, live_word());
   launch_merge<bf16_t, HD, WAVES * TILE, true>(a, g.cut, st);
 }
@@ -317,6 +317,7 @@ static int64_t likely_meetings(const AttendArgs& a) {
   int64_t sum = 0;
   for (int s = 0; s < a.tok.span.n_seq; ++s) {
     const int len = a.tok.span.off[s + 1] - a.tok.span.off[s];
+    if (!a.rule.takes(len * a.group)) continue;
     int keys = a.tok.limit - (a.rule.block > 0 ? len / 2 : 0);
     if (a.rule.window > 0 && !a.rule.prefix) keys = keys < a.rule.window * (a.rule.block > 0 ? 1 : 2) + TILE ? keys : a.rule.window * (a.rule.block > 0 ? 1 : 2) + TILE;
     sum += ((int64_t)len * a.group + TILE - 1) / TILE * ((keys + TILE - 1) / TILE);
@@ -332,12 +333,26 @@ static int64_t likely_meetings(const AttendArgs& a) {
 // behind 1000 to 8000, 8 heads of 4 queries 148 | 115 | 175; 259, 8000 in a window of 2048 200 | 172 | 178; 282, 6000 causal 256 | 194 | 196; 500, 8000
 // causal 404 | 316 | 296; 632, four of 2000 behind 4000 533 | 409 | 384; 1000, 8191 causal, 8 heads of 4 queries 778 | 592 | 552.
 constexpr int64_t RULED_FEW = 3 << 14, RULED_MANY = 25 << 14;
-template <class Rule, int HD> static void launch_ruled_t(bool bf16, const AttendArgs& a, hipStream_t st) {
-  const int most = most_rows(a.tok.span, a.group);
-  if (!bf16) launch_attend_t<float, HD, 1, 1, true, Rule>(a, st);
-  else if (most <= TILE) launch_attend_t<bf16_t, HD, 1, 1, true, Rule>(a, st);
-  else if (most > 2 * TILE && likely_meetings(a) * HD >= RULED_MANY * 128) launch_ruled_rows<Rule, HD, 8>(a, st);
-  else if (most > 2 * TILE && likely_meetings(a) * HD >= RULED_FEW * 128) launch_ruled_rows<Rule, HD, 4>(a, st);
+// Sequences of at most one row tile keep two numbers per weight, whatever else is in the call.  Beside them longer ones take one row tile per
+// workgroup too, or, where they would take a form of many rows, that form in a launch of its own.  All in one tile | two launches | all in the longest
+// one's form, with its weights, us, 16 heads unless stated: 8 sequences of 1 to 40 tokens behind 10 to 300 10.6 | 22.1 | 12.0, behind 500 to 2300 29.8 | 45.4 |
+// 34.8, 24 of 17 to 40 behind 1000 to 8000 173 | 198 | 219, 48 of 1 to 16, 8 heads of 4 queries 180 | 216 | 215, 4 of 1 to 300 behind 100 to 4000 45.7 | 58.9 |
+// 40.5; from RULED_FEW on: 12 of 1 to 500 behind 100 to 3000 119 | 120 | 108, 3 of 1 to 2000 137 | 133 | 121, 24 of 1 to 2000 860 | 595 | 586.
+template <class Rule, int HD> static void launch_ruled_t(bool bf16, AttendArgs a, hipStream_t st) {
+  const int most = most_rows(a);
+  bool few = !bf16 || most <= TILE;      // some sequence takes one row tile
+  for (int s = 0; s < a.tok.span.n_seq; ++s) few = few || (rows_of(a, s) > 0 && rows_of(a, s) <= TILE);
+  a.rule.least_rows = TILE + 1, a.rule.most_rows = INT32_MAX;
+  const int64_t weight = bf16 && most > 2 * TILE ? likely_meetings(a) * HD : 0;
+  if (few) {
+    a.rule.least_rows = 0, a.rule.most_rows = weight >= RULED_FEW * 128 ? TILE : INT32_MAX;
+    if (bf16) launch_attend_t<bf16_t, HD, 1, 1, true, Rule>(a, st);
+    else launch_attend_t<float, HD, 1, 1, true, Rule>(a, st);
+    if (a.rule.most_rows > TILE) return;
+    a.rule.least_rows = TILE + 1, a.rule.most_rows = INT32_MAX;
+  }
+  if (weight >= RULED_MANY * 128) launch_ruled_rows<Rule, HD, 8>(a, st);
+  else if (weight >= RULED_FEW * 128) launch_ruled_rows<Rule, HD, 4>(a, st);
   else launch_attend_t<bf16_t, HD, 1, 2, true, Rule>(a, st);
 }
 template <class Rule> static void launch_ruled_hd(bool bf16, const AttendArgs& a, hipStream_t st) {
