@@ -454,7 +454,7 @@ int dinfer_attend_ruled(dinfer_ctx* ctx, int32_t layer, int32_t n_seq, const int
  *   d_hold    [n_seq][n_rows] or null: >= 0: the hypothesis is finished, its only candidate is this token, at d_score[r].
  *   d_row, d_token [n_seq][n_keep] out: the candidates, best first; equal scores: the lower row, then the lower token.  Where there are
  *             fewer: -1 (d_score_out -infinity).
- *   d_score_out [n_seq][n_keep] out; may not be d_score.
+ *   d_score_out [n_seq][n_keep] out.  No output may be an input.
  *   d_scratch 256-byte aligned, dinfer_beam_scratch_bytes (0: a size out of range), contents irrelevant.
  * Scores are compared in 64 bits and rounded once, whatever the logits' size; a row's sum of exponentials is float32's, within 2^-20 of
  * itself.  (A score below float32's range is no candidate.  Thousands of candidates with one and the same score at the border of the best n_keep

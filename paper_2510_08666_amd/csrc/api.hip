@@ -1299,7 +1299,8 @@ int dinfer_beam_select(const void* d_logits, int32_t dtype, int64_t row_stride, 
   const int rc = check_select(n_seq, n_rows, vocab, n_keep);
   if (rc != DINFER_OK) return rc;
   if (row_stride < vocab || (uintptr_t)d_logits % (dtype == DINFER_BF16 ? 2 : 4)) return fail(DINFER_EINVAL, "rows %lld elements apart", (long long)row_stride);
-  if (d_score_out == d_score || d_row == d_token) return fail(DINFER_EINVAL, "an output is another argument");
+  if (d_score_out == d_score || d_row == d_token || (d_hold && (d_hold == d_row || d_hold == d_token || (const void*)d_hold == d_score_out)))
+    return fail(DINFER_EINVAL, "an output is another argument");
   if ((uintptr_t)d_scratch & 255) return fail(DINFER_EINVAL, "d_scratch must be 256-byte aligned");
   const size_t need = select_scratch_bytes((int64_t)n_seq * n_rows, vocab);
   if (scratch_bytes < need) return fail(DINFER_ENOSPACE, "scratch %zu < %zu bytes", scratch_bytes, need);
