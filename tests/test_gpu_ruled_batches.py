@@ -116,3 +116,27 @@ def test_odd_values_among_many_rows(cache_ops, call, rule_name):
             assert math.isnan(norm) and math.isnan(had) or abs(had - norm) <= e + 2.0 ** -21 * abs(norm), (r, h)
     assert finite > len(rows) * hd // 3      # (of twice that many)
     c.close()
+
+
+def test_two_launches_in_a_graph(cache_ops):
+    """Short sequences beside one of many rows, captured and replayed between eager calls on other queries: the eager result, bit for bit."""
+    c = cache_ops.Cache("bf16", 16, 128, [1, 2600, 7], [900, 300, 64], seed=6)
+    q, s, graph = c.randn(c.T, 2048), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    out, ref = (torch.zeros(c.T, 2048, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    run = lambda o: c.ctx.attend_ruled(0, c.lens, c.d_past, c.d_table, q, o, block=1)
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        run(out)
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph, stream=s):
+            run(out)
+    torch.cuda.synchronize()
+    for turn in range(4):
+        q.copy_(c.randn(c.T, 2048))
+        run(ref)
+        torch.cuda.synchronize()
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, ref) and out.abs().max() > 0, turn
+    c.close()
