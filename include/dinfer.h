@@ -427,7 +427,7 @@ int dinfer_refresh_block_scored(dinfer_ctx* ctx, int32_t n_seq, int32_t block_le
  *   block     0: e(p) has no bound (both directions).  b > 0: order in time by blocks of b positions behind the prefix, e(p) = the end of p's
  *             block: d_prefix[s] for p inside the prefix, else d_prefix[s] + ((p - d_prefix[s]) / b + 1) * b.  1: causal.
  *   window    0: no bound.
- *   d_prefix  [n_seq] or null (0): positions that all tokens of the sequence see, one another included.
+ *   d_prefix  [n_seq] or null (0): positions that all tokens of the sequence see, one another included.  Negative: taken as 0.
  *   d_first, d_end [T] or null (0 | all): the token's document, as cache positions.
  *   cap       0, or > 0: scores z become cap * tanh(z / cap), within 2^-20 of themselves whatever the cap.  At least 1e-30.
  *   d_slope   [n_q_heads] float32 or null: slope * |p - j| is taken off the head's scores (behind the cap). */
@@ -472,7 +472,7 @@ int dinfer_beam_select(const void* d_logits, int32_t dtype, int64_t row_stride, 
  *   d_parent  [n_new]: sequence i continues old sequence d_parent[i] (-1, or no old sequence: it begins empty).  Old sequences
  *             without children end.
  *   d_len, d_held [n_old]: their cached positions, and how many columns of their page-table rows they hold (at least what the positions
- *             take).
+ *             take).  Lengths beyond what a row of either page table or max_pos holds are cut to that.
  *   room      positions behind the cached ones that a new sequence gets pages for; rewrite: cached positions at its end that will
  *             be written again (0: none; a refreshed block's length, a vicinity's look_back).
  * With own = (len - rewrite, at least 0) / 16: columns in front of `own` are the parent's pages, shared.  Columns from `own` up to

@@ -245,7 +245,7 @@ struct TileWalk {
 // that a score far below its cap stays as it is; S's other coefficients make the largest relative error least (2^-26, by Lawson's weighted least
 // squares).  Beyond, cap - 2 cap / (exp(2u) + 1), which would cancel near 0.  Either is within 2^-21 of the score.  A score alone decides which one
 // it takes (so that no other one reaches it); a wave works out the second form where one of its scores needs it: prompts of 333 to
-// 1811 tokens in documents of 301 48.2 us without | 54.3 with it everywhere, 8191 causal tokens with 8 heads of 4 queries 732 | 1000 (uncapped 545).
+// 1811 tokens in documents of 301 48.2 us without | 54.3 with it everywhere, 8191 causal tokens with 8 heads of 4 queries 732 | 1000 (uncapped 540).
 struct CapScores {
   static constexpr double S[4] = {-0.333331438954662, 0.13325878934223193, -0.0530454923870277, 0.017241486995792973};
   // ratio: of a product to u, neither 0 nor infinite; unit: of a product to scores in log 2; small: S's coefficients, times unit

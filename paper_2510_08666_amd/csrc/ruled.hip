@@ -5,11 +5,11 @@
 //
 // Bound: the matrix instructions of the pairs that are seen (4 * head_dim operations each, at the 1.23 PFLOP/s of a large matrix product) or, for
 // few rows, one read of the keys and values.  Few rows take the kernel of attend_kernel.hpp with RangeRule for its words: a token behind
-// 511 positions 10.2 us (the chain of dependent loads), 48 tokens behind 1000 to 8000 in a window of 4097 with 8 heads of 4 queries 130 us (5.1 TB/s),
-// 512 tokens behind 4096, causal by blocks of 32, 39.9 us (0.46 PFLOP/s), prompts of 333 to 1811 tokens in documents of 301 with capped scores
-// 47 us (0.22 PFLOP/s: groups of rows in two documents walk both, all tiles partly seen, and end last).  Two row tiles hold their weights as one bfloat16 number (off by 2^-8 at most), which takes half
-// as many matrix instructions out of the product with the values: 47.0 -> 43.2 us and 63.6 -> 60.2 with the joins; one row tile waits for
-// memory and keeps two.  In tiles that are partly seen, values that are not finite are looked for only where an output has come out so, in a
+// 511 positions 10.4 us (the chain of dependent loads), 48 tokens behind 1000 to 8000 in a window of 4097 with 8 heads of 4 queries 130 us (5.1 TB/s),
+// 512 tokens behind 4096, causal by blocks of 32, 39.2 us (0.47 PFLOP/s), prompts of 333 to 1811 tokens in documents of 301 with capped scores
+// 48 us (0.21 PFLOP/s: groups of rows in two documents walk both, all tiles partly seen, and end last).  Two row tiles hold their weights as
+// one bfloat16 number (off by 2^-8 at most), which takes half as many matrix instructions out of the product with the values: 47.0 -> 43.2 us and
+// 63.6 -> 60.2 with the joins; one row tile waits for memory and keeps two.  In tiles that are partly seen, values that are not finite are looked for only where an output has come out so, in a
 // second walk: 60.3 -> 47.6 us for the documents, 43.9 -> 41.9 for the chunk.
 #include "attend_kernel.hpp"
 
@@ -26,7 +26,8 @@ namespace dinfer {
 // for two turns.  A workgroup alone on its compute unit takes 1800 cycles a turn, 512 of them its matrix instructions.
 // WAVES = 8: 256 rows, tiles of 64 keys, one workgroup per compute unit, and the two waves of a SIMD in two phases by barriers: one multiplies
 // while the other one does the rest, then they change places; a wave of the half that is behind still reads tile i while tile i + 3 comes in.
-// A causal prompt of 8191 tokens, 8 heads of 4 queries and 128 features: 544 us, 1.01 PFLOP/s (WAVES = 4: 595).  A phase of matrix work takes 1480
+// A causal prompt of 8191 tokens, 8 heads of 4 queries and 128 features: 530 to 550 us, 1.0 PFLOP/s (WAVES = 4: 595), the matrix units busy in 48 %
+// of the cycles.  A phase of matrix work takes 1480
 // cycles, 1024 of them the instructions' own, LDS gives 119 bytes a cycle, and the clock is 1.88 GHz.  Slower were: 4 waves of 32 rows with
 // the products of two tiles woven together (620 to 640 us); 64 rows per wave (842 and more, accumulators move between register files); half of the
 // values straight from L1 (813).

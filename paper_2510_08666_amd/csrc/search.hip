@@ -11,9 +11,9 @@ namespace dinfer {
 // once and leaves the maximum and the sum of exponentials of every chunk of 2048.  The second one, a workgroup per sequence, works
 // the rows' normalisers out of them, and a threshold: the n_keep-th best of the chunks' best candidates is no better than the n_keep-th
 // best candidate, so that only chunks that reach it, about n_keep of them, are read again, and what reaches it there is ranked, in 64 bits.
-// Bound: one read of the logits.  8 sequences of 64 rows of 157184 bfloat16, six rows of ten live (98 MB): the stream 19.7 us (5.0 TB/s), the join 17.0 (a chain of short
+// Bound: one read of the logits.  8 sequences of 64 rows of 157184 bfloat16, six rows of ten live (98 MB): the stream 20.7 us (4.7 TB/s), the join 16.6 (a chain of short
 // steps, 1024 threads: normalisers 4.5, the bound 2.4, the list of chunks 2.1, reading them 3.1, ranking 1.7); one launch that kept every
-// row's best ones as it went took 74.7.  4 rows of float32: 3.4 + 10.4.
+// row's best ones as it went took 74.7.  4 rows of float32: 3.4 + 10.7.
 constexpr int CHUNK_VALUES = 32, CHUNK = WAVE * CHUNK_VALUES;          // logits of a lane, in registers, and of a wave
 constexpr int SELECT_THREADS = 256, SELECT_WAVES = SELECT_THREADS / WAVE;
 constexpr uint32_t NO_VALUE = 0x007fffffu;                             // order_of(-inf): no candidate
@@ -601,7 +601,7 @@ __global__ __launch_bounds__(POOL_THREADS) void fork_plan_kernel(ForkArgs a) {
 }
 
 // The second: shared columns and the counts of all pages, the sequences' states, and the pages that are copied.  Bound by their bytes,
-// once each way: 64 sequences, 69 MB, 11.9 us.  (Workgroups that looked for themselves what to copy: 28.7 us both launches, with the list 25.0.)
+// once each way: 64 sequences, 69 MB, 12.3 us.  (Workgroups that looked for themselves what to copy: 28.7 us both launches, with the list 25.0.)
 __global__ __launch_bounds__(PIECE_THREADS) void fork_apply_kernel(ForkArgs a) {
   if (*a.missing > 0) return;
   const ForkGrid& g = a.grid;
